@@ -350,6 +350,185 @@ int kivi_decode_launches_ragged(const kivi_layout_t* layout, const kivi_seq_stat
  */
 int kivi_stream_read_probe(const void* src, size_t bytes, void* sink, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Operators around the cache: per-head norms with the position rotation, attention of prompts, and a
+ * paged form of the cache whose lengths and pages are device data, with its append and its attention.
+ * The conventions above hold: status codes, validation on the host before anything is enqueued, no
+ * allocation, the caller's stream.  What lies in device memory (positions, starts, lengths, page numbers,
+ * slots) cannot be validated there; what the kernels do with values out of range stands with each call, and no
+ * such value makes them read or write outside the buffers they were given.  All of these calls can be
+ * recorded into a HIP graph; a replay reads the device data as it is then.
+ * ---------------------------------------------------------------------------------------------- */
+
+/* element types of tensors that are not bound to fp16 */
+#define KIVI_TYPE_FP16          0
+#define KIVI_TYPE_BF16          1
+
+/* A tensor of 16-bit elements: element (b, h, t, c), c < 128, at data[b*stride_b + h*stride_h + t*stride_t + c]
+ * (strides in elements, multiples of 8, not negative; data 16-byte aligned).  Tensors of rows use t as the
+ * row and b = 0. */
+typedef struct kivi_tensor {
+    void *data;
+    int64_t stride_b, stride_h, stride_t;
+} kivi_tensor_t;
+
+/* Position rotation: channel pair i of a head at position p becomes
+ * (x cos - y sin, y cos + x sin) with cos = table[p][i], sin = table[p][rotary_dim/2 + i]. */
+typedef struct kivi_rotation {
+    const float *table;         /* device, fp32 [n_positions][rotary_dim], 16-byte aligned            */
+    const int32_t *positions;   /* device, one position per row; where it may be NULL stands with the  */
+                                /* call.  Positions outside the table are taken as its nearest end     */
+    int32_t n_positions;        /* >= 1                                                                */
+    int32_t rotary_dim;         /* channels that rotate, the first ones: a multiple of 16, 16 to 128   */
+    int32_t interleaved;        /* 0: channels i and i + rotary_dim/2 are a pair; 1: 2i and 2i + 1     */
+} kivi_rotation_t;
+
+/* One tensor of kivi_norm_rotate. */
+typedef struct kivi_norm_rotate_job {
+    kivi_tensor_t src, dst;     /* [row][n_heads][128]; dst may be src (same data and strides)         */
+    const void *weight;         /* device, [128] in src's type, 16-byte aligned; NULL: no norm         */
+    float weight_offset;        /* added to the weight (0, or 1 for weights stored as w - 1)           */
+    int32_t n_heads;
+    int32_t src_type, dst_type; /* KIVI_TYPE_*                                                         */
+} kivi_norm_rotate_job_t;
+
+/*
+ * Norms of every head and the position rotation in one pass over up to two tensors (queries and keys of the
+ * same rows), one launch:
+ *   y = x / sqrt(mean(x^2) + eps) * (weight + weight_offset)      (weight non-NULL)
+ *   dst = y rotated by its row's position                          (rotation non-NULL)
+ * in fp32, rounded once to dst's type.
+ *   rotation->positions   required: one per row
+ * Errors: INVALID_ARG (null, misaligned, n_jobs not 1 or 2, counts, eps < 0 or not finite), UNSUPPORTED
+ * (types, rotary_dim), HIP.  No rows: OK without a launch.
+ */
+int kivi_norm_rotate(const kivi_norm_rotate_job_t* jobs, int32_t n_jobs, int32_t n_rows, float eps,
+                     const kivi_rotation_t* rotation, void* stream);
+
+/* Attention of prompts. */
+typedef struct kivi_prompt {
+    int32_t batch, n_q_heads, n_kv_heads, head_dim;   /* head_dim 128; n_q_heads a multiple of n_kv_heads */
+    int32_t type;               /* of q, k, v and out                                                  */
+    int32_t max_q, max_k;       /* queries and keys of every sequence (starts NULL), or of the longest */
+    const int32_t *q_starts;    /* device [batch + 1], or NULL: the queries of sequence b are the rows   */
+    const int32_t *k_starts;    /* t = starts[b] .. starts[b+1] - 1 (with b = 0), its keys likewise      */
+    int32_t q_rows, k_rows;     /* rows of q and out, of k and v (starts non-NULL)                     */
+    int32_t window;             /* 0, or the number of latest keys that a query sees, itself included   */
+    int32_t sinks;              /* first keys that stay visible behind the window                       */
+    float softmax_scale;
+} kivi_prompt_t;
+
+/* Host helper: bytes of workspace with which kivi_prompt_attention may split long key ranges over workgroups where
+ * a call has few queries (0: it would not).  Errors: as kivi_prompt_attention. */
+int kivi_prompt_workspace_bytes(const kivi_prompt_t* prompt, size_t* bytes);
+
+/*
+ * Attention of a prompt's (or its last chunk's) queries over its keys in 16 bits -- what precedes Algorithm 1
+ * (Prefill).  The last query of a sequence meets its last key: query i of n_q stands at p = n_k - n_q + i and
+ * sees key j when j <= p and (window == 0 or p - j < window or j < sinks).  Rows that see nothing (p < 0)
+ * become 0.  Query head j reads kv-head j / (n_q_heads / n_kv_heads).  Logits, softmax and sums are fp32;
+ * probabilities meet the values in the tensors' type.
+ *   workspace       device scratch, or NULL.  Contents need not be kept or cleared; calls that overlap must not share it.
+ * A sequence whose starts decrease, are outside the rows or are further apart than max_q / max_k is left out.  Rows of out
+ * that belong to no sequence are left as they are.
+ * Keys and values of a sequence have to be finite; what lies behind a sequence's end is not read.
+ * Errors: INVALID_ARG, UNSUPPORTED (head_dim, type), WORKSPACE (given, but smaller than kivi_prompt_workspace_bytes), HIP.
+ */
+int kivi_prompt_attention(const kivi_prompt_t* prompt, const kivi_tensor_t* q, const kivi_tensor_t* k,
+                          const kivi_tensor_t* v, const kivi_tensor_t* out, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/*
+ * The paged cache (policy KIVI_FLUSH_WINDOW, G = 32).  Of a sequence of n tokens the first
+ * floor(max(n - R, 0) / 32) * 32 are packed, the others are fp16 rows: its state follows from its length, which is
+ * device data.
+ *   pages    [n_pages][n_kv_heads][page_tokens / 32][record]: a record holds 32 tokens of one kv-head,
+ *            key codes (one key tile as above), k_scale fp16 [128], k_zero fp16 [128], v_scale fp16 [32][4], v_zero
+ *            fp16 [32][4], value codes (one value tile): 1024 + 2048 * B / 2 bytes
+ *   k_resid, v_resid   fp16 [max_sequences][n_kv_heads][cap_r_tokens][128]: token t in slot t % cap_r_tokens
+ */
+typedef struct kivi_paged_layout {
+    int32_t max_sequences;      /* sequences that the fp16 rows have room for                          */
+    int32_t n_q_heads, n_kv_heads, head_dim;    /* 1 to 128 query heads per kv-head; head_dim 128        */
+    int32_t bits;               /* 2 or 4                                                              */
+    int32_t group;              /* 32                                                                  */
+    int32_t residual;           /* R, a multiple of 32                                                 */
+    int32_t page_tokens;        /* a power of two, 32 to 4096                                          */
+    int32_t n_pages;
+    int32_t cap_r_tokens;       /* a multiple of 32, >= R + 32                                         */
+} kivi_paged_layout_t;
+
+typedef struct kivi_paged_cache {
+    void *pages, *k_resid, *v_resid;            /* device, 16-byte aligned; sizes: kivi_paged_sizes     */
+} kivi_paged_cache_t;
+
+typedef struct kivi_paged_sizes {
+    size_t pages, k_resid, v_resid;
+    size_t workspace;           /* of kivi_paged_attention, whatever the batch                         */
+} kivi_paged_sizes_t;
+
+/* The sequences of a call; the arrays are device memory. */
+typedef struct kivi_paged_batch {
+    int32_t batch;
+    int32_t max_pages;          /* entries of a row of page_table                                      */
+    int64_t page_table_stride;  /* from row to row, >= max_pages                                       */
+    const int32_t *page_table;  /* [batch][max_pages]: entry i is the page of tokens i * page_tokens ..  */
+    const int32_t *lengths;     /* [batch]: tokens, those of this step included                        */
+    const int32_t *slots;       /* [batch]: which fp16 rows are the sequence's; NULL: sequence b has b   */
+} kivi_paged_batch_t;
+
+/* New rows for kivi_paged_append. */
+typedef struct kivi_paged_rows {
+    kivi_tensor_t k, v;         /* [row][n_kv_heads][128] in `type`                                    */
+    kivi_tensor_t q;            /* [row][n_q_heads][128] in `type`, rotated into q_out (fp16); data     */
+    kivi_tensor_t q_out;        /* NULL in both: no queries                                            */
+    int32_t type;
+    int32_t n_rows;             /* rows of these tensors and of rotation->positions                    */
+    int32_t max_new;            /* new tokens of every sequence (starts NULL), or of the longest       */
+    const int32_t *starts;      /* device [batch + 1], or NULL: rows starts[b] .. starts[b+1] - 1 are the last tokens */
+                                /* of sequence b; NULL: rows b * max_new .. (b + 1) * max_new - 1       */
+    const kivi_rotation_t *rotation;    /* of k and q, or NULL; its positions may be NULL: the token's place in its sequence */
+} kivi_paged_rows_t;
+
+/* Host helper: byte sizes for a layout.  Errors: INVALID_ARG, UNSUPPORTED. */
+int kivi_paged_sizes(const kivi_paged_layout_t* layout, kivi_paged_sizes_t* sizes);
+
+/*
+ * Append the new tokens of every sequence to the paged cache: rotate keys (and queries) on the way, quantise the
+ * groups that leave the window (Section 3.3, formula of Section 3.1, the contract above) out of the fp16 rows or straight out of
+ * the new ones, and store the rows that stay.  lengths[b] counts the new tokens already.  Keys are rotated in fp32, each
+ * product and the difference rounded on its own, and rounded to fp16 once; these fp16 numbers are what is quantised.
+ *   A sequence whose rows are outside [0, n_rows), whose count of them is negative, above max_new or above lengths[b], or whose slot
+ *   is outside [0, max_sequences), is left as it is, its queries too.  Groups whose page is outside the table or [0, n_pages) are not
+ *   stored.  No two sequences of a call may share a slot or a page that is written.
+ * One launch, two where a call may read fp16 rows that it also replaces (max_new > cap_r_tokens - R - 31).
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ */
+int kivi_paged_append(const kivi_paged_layout_t* layout, const kivi_paged_cache_t* cache, const kivi_paged_batch_t* batch,
+                      const kivi_paged_rows_t* rows, void* stream);
+
+/* One attention call over the paged cache. */
+typedef struct kivi_paged_query {
+    const void *q;              /* device, fp16 [batch][n_q_heads][128]                                */
+    void *out;                  /* device, [batch][n_q_heads][128] in out_type                         */
+    int32_t out_type;           /* KIVI_TYPE_*                                                         */
+    int32_t window, sinks;      /* as for kivi_prompt_attention, for the token at lengths[b] - 1       */
+    float softmax_scale;
+} kivi_paged_query_t;
+
+/*
+ * Attention of one token per sequence over the paged cache: Equation 4 and Algorithm 1 (Decoding) as in
+ * kivi_decode_attention, for sequences of any lengths in one launch that divides the visible records evenly over
+ * the device.
+ *   workspace   device scratch of kivi_paged_sizes' bytes, zero-filled once before its first use; every call
+ *               leaves it ready for the next one.  Calls that overlap (two streams, two graphs) must not share it.
+ * Rows of `out` of sequences with lengths[b] < 1 or a slot outside [0, max_sequences) are left as they are.  Records whose
+ * page is outside the table or [0, n_pages) count as masked; a row that sees nothing at all becomes 0.
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.
+ */
+int kivi_paged_attention(const kivi_paged_layout_t* layout, const kivi_paged_cache_t* cache, const kivi_paged_batch_t* batch,
+                         const kivi_paged_query_t* query, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

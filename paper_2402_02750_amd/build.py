@@ -14,7 +14,8 @@ LIB_PATH = os.path.join(PKG_DIR, "libkivi_hip.so")
 
 SOURCES = ["kivi_api.hip", "kivi_quantize.hip", "kivi_decode_valu.hip", "kivi_decode_mfma.hip",
            "kivi_decode_tiles.hip", "kivi_decode_one.hip", "kivi_decode_rows.hip",
-           "kivi_ragged_rows.hip"]
+           "kivi_ragged_rows.hip", "kivi_operators_api.hip", "kivi_norm_rotate.hip", "kivi_prompt_attention.hip",
+           "kivi_paged_append.hip", "kivi_paged_attention.hip"]
 
 COMMON_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextra",
@@ -29,6 +30,7 @@ PER_FILE_FLAGS = {
     "kivi_quantize.hip": ["-ffp-contract=off"],
     "kivi_decode_one.hip": ["-ffp-contract=off"],       # quantises the tokens of a flush
     "kivi_ragged_rows.hip": ["-ffp-contract=off"],      # the same
+    "kivi_paged_append.hip": ["-ffp-contract=off"],     # the same, and the rotation of the keys before it
 }
 
 

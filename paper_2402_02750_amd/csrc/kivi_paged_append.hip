@@ -1,0 +1,236 @@
+// Append to the paged cache (kivi_paged_append): rotation on the way, quantisation of the groups that leave the window, and the fp16
+// rows that stay.
+//
+// A sequence's state follows from its length, so every wavefront works out from lengths[b] and the number of new rows
+// what there is for it to do.  Two roles:
+//   groups  one wavefront per (sequence, group that leaves the window in this call, kv-head, keys or values): loads its 32 tokens out of
+//           the fp16 rows or the new ones, rotates the new keys and quantises in registers (kivi_quantize_tile.h)
+//   rows    one wavefront per (sequence, new token, eight heads of q, k and v): rotates, and stores queries, and keys and
+//           values of tokens that stay in the window
+// The roles do not wait for each other.  Rows are stored at slot t % cap_r, groups read slots of tokens before the call: the first read
+// is at most n + R + 30 tokens before the last one written, so one launch is right while that is less than cap_r; otherwise
+// the rows are a launch after the groups.
+//
+// The packed codes are a bit contract, so the rotation is one too: fp32 products and one difference, each rounded on its own
+// (this file is compiled without contraction), then one rounding to fp16.
+#include "kivi_paged.h"
+#include "kivi_quantize_tile.h"
+
+#include <algorithm>
+
+namespace kivi {
+namespace {
+
+using namespace head_rows;
+using tile::half2v;
+
+struct Args : PagedAppendParams {
+    int32_t group_blocks;              // workgroups of the first role
+    int32_t groups, tokens, pieces;    // per sequence: groups, tokens looked at; per token: runs of eight heads
+    int64_t group_waves, row_waves;
+};
+
+struct Sequence {
+    int before, after, first_row, slot;            // tokens before and after the call; the row of its first new token
+    bool valid;
+};
+__device__ __forceinline__ Sequence sequence_of(const Args& p, int b) {
+    Sequence s;
+    s.after = p.lengths[b];
+    const int64_t row0 = p.starts ? p.starts[b] : (int64_t)b * p.max_new;
+    const int64_t n = p.starts ? (int64_t)p.starts[b + 1] - row0 : p.max_new;
+    s.slot = p.slots ? p.slots[b] : b;
+    s.valid = n >= 0 && n <= p.max_new && n <= s.after && row0 >= 0 && row0 + n <= p.n_rows && s.slot >= 0 && s.slot < p.max_sequences;
+    s.before = s.after - (int)n;
+    s.first_row = (int)row0;
+    return s;
+}
+
+// Channels 2 lane, 2 lane + 1 of a row of `bits16` after the rotation, from the row's raw pairs; `partner`: the pair of the lane
+// that holds the other channels
+__device__ __forceinline__ half2v turned_pair(const RotationParams& r, uint32_t raw, bool bf16, bool rotates, int position, int lane) {
+    auto pair_of = [&](uint32_t w, float& x, float& y) {
+        if (bf16) {
+            x = __uint_as_float(w << 16);
+            y = __uint_as_float(w & 0xFFFF0000u);
+        } else {
+            x = (float)tile::as_half2(w).x;
+            y = (float)tile::as_half2(w).y;
+        }
+    };
+    float x, y;
+    pair_of(raw, x, y);
+    if (rotates) {
+        const float* row = r.table + (int64_t)position * (2 * r.half);
+        const int c = 2 * lane;
+        if (r.interleaved) {
+            if (c < 2 * r.half) turn_pair(x, y, row[lane], row[r.half + lane]);
+        } else {
+            const bool low = c < r.half, turns = c < 2 * r.half;
+            const int other = turns ? (low ? lane + r.half / 2 : lane - r.half / 2) : lane;
+            float px, py;
+            pair_of((uint32_t)__shfl((int)raw, other), px, py);
+            if (turns) {
+                const int i = low ? c : c - r.half;
+                const float2 cs = *reinterpret_cast<const float2*>(row + i), sn = *reinterpret_cast<const float2*>(row + r.half + i);
+                // (x cos - y sin, y cos + x sin): this lane has the first or the second of the pair
+                const float x0 = low ? x : px, x1 = low ? y : py;
+                float y0 = low ? px : x, y1 = low ? py : y, a0 = x0, a1 = x1;
+                turn_pair(a0, y0, cs.x, sn.x);
+                turn_pair(a1, y1, cs.y, sn.y);
+                x = low ? a0 : y0;
+                y = low ? a1 : y1;
+            }
+        }
+    }
+    half2v h;
+    h.x = (_Float16)x;
+    h.y = (_Float16)y;
+    return h;
+}
+
+template <int BITS>
+__device__ __forceinline__ void group_role(const Args& p, int64_t at, int lane) {
+    const int kv = (int)(at & 1);
+    at >>= 1;
+    const int h = (int)(at % p.n_kv_heads);
+    at /= p.n_kv_heads;
+    const int g = (int)(at % p.groups), b = (int)(at / p.groups);
+    const Sequence s = sequence_of(p, b);
+    const int record = packed_records(s.before, p.residual) + g;
+    if (!s.valid || record >= packed_records(s.after, p.residual)) return;
+    const int entry = record >> p.page_shift;
+    if (entry >= p.max_pages) return;
+    const int page = p.page_table[b * p.page_table_stride + entry];
+    if (page < 0 || page >= p.n_pages) return;
+    char* rec = p.pages + (((((int64_t)page * p.n_kv_heads + h) << p.page_shift) + (record & ((1 << p.page_shift) - 1))) * record_bytes(BITS));
+    constexpr int kWords = kTileTokens * kHeadDim * BITS / 32;
+    uint32_t* words = reinterpret_cast<uint32_t*>(rec);
+    const int t0 = record * kTileTokens;
+    const __half* ring = (kv ? p.v_resid : p.k_resid) + ((int64_t)s.slot * p.n_kv_heads + h) * p.cap_r * kHeadDim;
+    const TensorParams& fresh = kv ? p.v : p.k;
+    const __half* rows = fresh.data + (int64_t)h * fresh.stride_h + (int64_t)s.first_row * fresh.stride_t;
+    int slot0 = t0 % p.cap_r;
+    auto row_at = [&](int i) -> const __half* {                // of token t0 + i
+        const int t = t0 + i, slot = slot0 + i - (slot0 + i >= p.cap_r ? p.cap_r : 0);
+        return t < s.before ? ring + slot * kHeadDim : rows + (int64_t)(t - s.before) * fresh.stride_t;
+    };
+    if (!kv) {
+        uint32_t raw[kTileTokens];
+        half2v x[kTileTokens];
+#pragma unroll
+        for (int i = 0; i < kTileTokens; ++i) raw[i] = *reinterpret_cast<const uint32_t*>(row_at(i) + 2 * lane);
+#pragma unroll
+        for (int i = 0; i < kTileTokens; ++i) {
+            const bool is_new = t0 + i >= s.before;
+            x[i] = tile::as_half2(raw[i]);
+            if (is_new && (p.bf16 || p.rotates)) {
+                int position = t0 + i;
+                if (p.rotates) position = clamped_position(p.rotation, p.rotation.positions ? p.rotation.positions[s.first_row + t0 + i - s.before] : position);
+                x[i] = turned_pair(p.rotation, raw[i], p.bf16, p.rotates, position, lane);
+            }
+        }
+        half2v* scales = reinterpret_cast<half2v*>(words + kWords);
+        tile::quantize_key_tile<BITS>(x, lane,
+            [&](half2v s2, half2v z2) {
+                scales[lane] = s2;
+                scales[64 + lane] = z2;
+            },
+            [&](int i, uint32_t w) { words[i] = w; });
+    } else {
+        tile::ValueRow x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i].v4 = *reinterpret_cast<const tile::uint4v*>(row_at((lane >> 4) * 8 + i) + (lane & 15) * 8);
+        if (p.bf16) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (t0 + (lane >> 4) * 8 + i >= s.before) {
+                    float f[8];
+                    to_floats(x[i].v4, true, f);
+                    x[i].v4 = from_floats(f, false);
+                }
+        }
+        _Float16* scales = reinterpret_cast<_Float16*>(words + kWords + 128);
+        tile::quantize_value_tile<BITS>(x, lane,
+            [&](int i, _Float16 sc, _Float16 z) {
+                scales[i] = sc;
+                scales[128 + i] = z;
+            },
+            [&](int i, uint32_t w) { words[kWords + 256 + i] = w; });
+    }
+}
+
+__device__ __forceinline__ void row_role(const Args& p, int64_t at, int lane) {
+    const int piece = (int)(at % p.pieces);
+    at /= p.pieces;
+    const int from_end = (int)(at % p.tokens), b = (int)(at / p.tokens);
+    const Sequence s = sequence_of(p, b);
+    const int t = s.after - 1 - from_end;              // its place in the sequence
+    if (!s.valid || t < s.before) return;
+    const bool stays = t >= packed_records(s.after, p.residual) * kTileTokens;
+    const int n_q = p.q_out.data ? p.n_q_heads : 0, head = piece * 8 + (lane >> 3), j = lane & 7;
+    const int64_t row = (int64_t)s.first_row + t - s.before;
+    const bool is_q = head < n_q, is_k = !is_q && head < n_q + p.n_kv_heads;
+    if (head >= n_q + 2 * p.n_kv_heads || (!is_q && !stays)) return;
+    const TensorParams& from = is_q ? p.q : is_k ? p.k : p.v;
+    const int h = is_q ? head : is_k ? head - n_q : head - n_q - p.n_kv_heads;
+    const __half* src = from.data + row * from.stride_t + h * from.stride_h;
+    __half* dst;
+    if (is_q) dst = p.q_out.data + row * p.q_out.stride_t + h * p.q_out.stride_h;
+    else dst = (is_k ? p.k_resid : p.v_resid) + (((int64_t)s.slot * p.n_kv_heads + h) * p.cap_r + t % p.cap_r) * kHeadDim;
+    const Pieces pc = pieces_of(j, p.rotates ? p.rotation.half : 0, p.rotation.interleaved);
+    uint4v a4 = *reinterpret_cast<const uint4v*>(src + pc.a * 8), b4 = *reinterpret_cast<const uint4v*>(src + pc.b * 8);
+    const bool turns = p.rotates && (is_q || is_k) && j < p.rotation.half / 8;
+    if (turns || p.bf16) {
+        float x[8], y[8];
+        to_floats(a4, p.bf16, x);
+        to_floats(b4, p.bf16, y);
+        if (turns) {
+            Turn turn;
+            load_turn(p.rotation, clamped_position(p.rotation, p.rotation.positions ? p.rotation.positions[row] : t), j, turn);
+            turn_pieces(x, y, turn, p.rotation.interleaved);
+        }
+        a4 = from_floats(x, false);
+        b4 = from_floats(y, false);
+    }
+    *reinterpret_cast<uint4v*>(dst + pc.a * 8) = a4;
+    *reinterpret_cast<uint4v*>(dst + pc.b * 8) = b4;
+}
+
+template <int BITS>
+__global__ __launch_bounds__(256) void paged_append_kernel(Args p) {
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if ((int)blockIdx.x < p.group_blocks) {
+        const int64_t at = (int64_t)blockIdx.x * 4 + wave;
+        if (at < p.group_waves) group_role<BITS>(p, at, lane);
+    } else {
+        const int64_t at = (int64_t)((int)blockIdx.x - p.group_blocks) * 4 + wave;
+        if (at < p.row_waves) row_role(p, at, lane);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_paged_append(const PagedAppendParams& params, hipStream_t stream) {
+    Args p{};
+    static_cast<PagedAppendParams&>(p) = params;
+    p.groups = (p.max_new + kTileTokens - 1) / kTileTokens;
+    const int window = p.residual + kTileTokens - 1;            // rows that stay, at most
+    p.tokens = p.q_out.data ? p.max_new : std::min(p.max_new, window);
+    p.pieces = ((p.q_out.data ? p.n_q_heads : 0) + 2 * p.n_kv_heads + 7) / 8;
+    p.group_waves = (int64_t)p.batch * p.groups * p.n_kv_heads * 2;
+    p.row_waves = (int64_t)p.batch * p.tokens * p.pieces;
+    const int64_t group_blocks = (p.group_waves + 3) / 4, row_blocks = (p.row_waves + 3) / 4;
+    if (group_blocks + row_blocks > 0x7fffffff) return hipErrorInvalidValue;
+    auto launch = [&](int64_t groups, int64_t rows) {
+        p.group_blocks = (int32_t)groups;
+        if (p.bits == 2) paged_append_kernel<2><<<(unsigned)(groups + rows), 256, 0, stream>>>(p);
+        else paged_append_kernel<4><<<(unsigned)(groups + rows), 256, 0, stream>>>(p);
+        return hipGetLastError();
+    };
+    if ((int64_t)p.max_new + p.residual + 30 < p.cap_r) return launch(group_blocks, row_blocks);
+    if (hipError_t e = launch(group_blocks, 0); e != hipSuccess) return e;
+    return launch(0, row_blocks);
+}
+
+}  // namespace kivi

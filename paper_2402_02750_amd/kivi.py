@@ -24,6 +24,8 @@ KIVI_DECODE_VALU = 1
 KIVI_DECODE_MFMA = 2
 KIVI_DECODE_MFMA_ONE = 3
 KIVI_DECODE_MFMA_TWO = 4
+KIVI_TYPE_FP16 = 0
+KIVI_TYPE_BF16 = 1
 
 EXPORTS = [
     "kivi_status_string", "kivi_cache_sizes", "kivi_decode_workspace_bytes", "kivi_decode_plan",
@@ -31,6 +33,8 @@ EXPORTS = [
     "kivi_flush_residual", "kivi_decode_attention", "kivi_decode_step", "kivi_stream_read_probe",
     "kivi_batch_slice", "kivi_decode_step_ragged", "kivi_decode_attention_ragged",
     "kivi_decode_attention_static", "kivi_decode_launches_ragged",
+    "kivi_norm_rotate", "kivi_prompt_workspace_bytes", "kivi_prompt_attention", "kivi_paged_sizes",
+    "kivi_paged_append", "kivi_paged_attention",
 ]
 KIVI_STATIC_WORKSPACE_BYTES = 8 << 20
 
@@ -66,6 +70,56 @@ class kivi_decode_plan_t(ctypes.Structure):
 class kivi_cache_sizes_t(ctypes.Structure):
     _fields_ = [(n, ctypes.c_size_t) for n in (
         "k_codes", "k_scale", "k_zero", "v_codes", "v_scale", "v_zero", "k_resid", "v_resid")]
+
+
+class kivi_tensor_t(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p)] + [(n, ctypes.c_int64) for n in ("stride_b", "stride_h", "stride_t")]
+
+
+class kivi_rotation_t(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("positions", ctypes.c_void_p)] + \
+        [(n, ctypes.c_int32) for n in ("n_positions", "rotary_dim", "interleaved")]
+
+
+class kivi_norm_rotate_job_t(ctypes.Structure):
+    _fields_ = [("src", kivi_tensor_t), ("dst", kivi_tensor_t), ("weight", ctypes.c_void_p), ("weight_offset", ctypes.c_float)] + \
+        [(n, ctypes.c_int32) for n in ("n_heads", "src_type", "dst_type")]
+
+
+class kivi_prompt_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_q_heads", "n_kv_heads", "head_dim", "type", "max_q", "max_k")] + \
+        [("q_starts", ctypes.c_void_p), ("k_starts", ctypes.c_void_p)] + \
+        [(n, ctypes.c_int32) for n in ("q_rows", "k_rows", "window", "sinks")] + [("softmax_scale", ctypes.c_float)]
+
+
+class kivi_paged_layout_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "max_sequences", "n_q_heads", "n_kv_heads", "head_dim", "bits", "group", "residual",
+        "page_tokens", "n_pages", "cap_r_tokens")]
+
+
+class kivi_paged_cache_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("pages", "k_resid", "v_resid")]
+
+
+class kivi_paged_sizes_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_size_t) for n in ("pages", "k_resid", "v_resid", "workspace")]
+
+
+class kivi_paged_batch_t(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("page_table_stride", ctypes.c_int64)] + \
+        [(n, ctypes.c_void_p) for n in ("page_table", "lengths", "slots")]
+
+
+class kivi_paged_rows_t(ctypes.Structure):
+    _fields_ = [(n, kivi_tensor_t) for n in ("k", "v", "q", "q_out")] + \
+        [(n, ctypes.c_int32) for n in ("type", "n_rows", "max_new")] + \
+        [("starts", ctypes.c_void_p), ("rotation", ctypes.POINTER(kivi_rotation_t))]
+
+
+class kivi_paged_query_t(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("out", ctypes.c_void_p)] + \
+        [(n, ctypes.c_int32) for n in ("out_type", "window", "sinks")] + [("softmax_scale", ctypes.c_float)]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -106,6 +160,13 @@ def load_library() -> ctypes.CDLL:
                                             ctypes.c_float, I32, VP, VP, ctypes.c_size_t, VP]
     lib.kivi_decode_attention_ragged.argtypes = [P(kivi_layout_t), P(kivi_cache_t), P(kivi_seq_state_t), VP,
                                                  ctypes.c_float, VP, VP, ctypes.c_size_t, VP]
+    lib.kivi_norm_rotate.argtypes = [P(kivi_norm_rotate_job_t), I32, I32, ctypes.c_float, P(kivi_rotation_t), VP]
+    lib.kivi_prompt_workspace_bytes.argtypes = [P(kivi_prompt_t), P(ctypes.c_size_t)]
+    lib.kivi_prompt_attention.argtypes = [P(kivi_prompt_t)] + [P(kivi_tensor_t)] * 4 + [VP, ctypes.c_size_t, VP]
+    lib.kivi_paged_sizes.argtypes = [P(kivi_paged_layout_t), P(kivi_paged_sizes_t)]
+    lib.kivi_paged_append.argtypes = [P(kivi_paged_layout_t), P(kivi_paged_cache_t), P(kivi_paged_batch_t), P(kivi_paged_rows_t), VP]
+    lib.kivi_paged_attention.argtypes = [P(kivi_paged_layout_t), P(kivi_paged_cache_t), P(kivi_paged_batch_t), P(kivi_paged_query_t),
+                                         VP, ctypes.c_size_t, VP]
     for name in EXPORTS[1:]:
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
@@ -343,3 +404,197 @@ def kivi_decode_attention_ragged(layout, cache: Cache, states, q_fp16, softmax_s
         ctypes.c_void_p(cache.workspace.data_ptr()), cache.workspace.numel(), _stream_handle(stream)),
         "kivi_decode_attention_ragged")
     return out_fp32
+
+
+# ---- operators around the cache ----
+
+def _type_of(x) -> int:
+    import torch
+    if x.dtype == torch.float16:
+        return KIVI_TYPE_FP16
+    if x.dtype == torch.bfloat16:
+        return KIVI_TYPE_BF16
+    raise KiviError(KIVI_ERR_UNSUPPORTED, f"tensor of {x.dtype}")
+
+
+def _on_device(*tensors):
+    """All tensors on the current device: its stream and launches are the ones the library uses."""
+    import torch
+    here = torch.cuda.current_device()
+    for x in tensors:
+        if x is not None and (not x.is_cuda or x.device.index != here):
+            raise KiviError(KIVI_ERR_INVALID_ARG, f"tensor on {x.device}, the current device is cuda:{here}")
+
+
+def _rows(x, heads=None, rows=None):
+    """[rows, heads, 128] (any row and head strides) as a kivi_tensor_t."""
+    assert x.dim() == 3 and x.shape[2] == 128 and x.stride(2) == 1, "expected [rows, heads, 128] with contiguous channels"
+    assert (heads is None or x.shape[1] == heads) and (rows is None or x.shape[0] == rows), f"unexpected shape {tuple(x.shape)}"
+    return kivi_tensor_t(x.data_ptr(), 0, x.stride(1), x.stride(0))
+
+
+def _int32(x, n=None):
+    """Device pointer of a contiguous int32 tensor (None: null)."""
+    if x is None:
+        return None
+    import torch
+    assert x.dtype == torch.int32 and x.is_contiguous() and (n is None or x.numel() >= n), "expected a contiguous int32 tensor"
+    return x.data_ptr()
+
+
+class Rotation:
+    """A table of cosines and sines for the position rotation: CUDA fp32 [n_positions, rotary_dim], the cosines of the
+    rotary_dim / 2 channel pairs first.  interleaved: pairs are neighbouring channels."""
+
+    def __init__(self, table, interleaved=False):
+        import torch
+        assert table.dim() == 2 and table.dtype == torch.float32 and table.is_contiguous(), "expected a contiguous fp32 table"
+        self.table = table
+        self.interleaved = int(interleaved)
+
+    def c(self, positions=None, rows=0) -> kivi_rotation_t:
+        return kivi_rotation_t(self.table.data_ptr(), _int32(positions, rows), self.table.shape[0], self.table.shape[1], self.interleaved)
+
+
+def kivi_norm_rotate(q, q_out, k=None, k_out=None, q_weight=None, k_weight=None, eps=1e-6, weight_offset=0.0,
+                     rotation: Optional[Rotation] = None, positions=None, stream=None):
+    """q, k: CUDA fp16 / bf16 [rows, heads, 128] (any row and head strides); q_out, k_out the same shapes, fp16 or bf16, maybe q
+    and k themselves; weights: [128] in the type of q / k, or None (no norm); positions: int32 [rows]."""
+    _on_device(q, q_out, k, k_out, q_weight, k_weight, positions, rotation.table if rotation else None)
+    rows = q.shape[0]
+    jobs = (kivi_norm_rotate_job_t * 2)()
+    n = 0
+    for x, y, w in ((q, q_out, q_weight), (k, k_out, k_weight)):
+        if x is None:
+            continue
+        assert w is None or (w.dtype == x.dtype and w.numel() == 128 and w.is_contiguous()), "expected a weight [128] of the tensor's type"
+        jobs[n] = kivi_norm_rotate_job_t(_rows(x, rows=rows), _rows(y, x.shape[1], rows), w.data_ptr() if w is not None else None,
+                                         weight_offset, x.shape[1], _type_of(x), _type_of(y))
+        n += 1
+    r = None
+    if rotation is not None:
+        assert positions is not None, "a rotation needs positions"
+        r = ctypes.byref(rotation.c(positions, rows))
+    _check(load_library().kivi_norm_rotate(jobs, n, rows, eps, r, _stream_handle(stream)), "kivi_norm_rotate")
+
+
+def kivi_prompt_attention(q, k, v, out, softmax_scale, q_starts=None, k_starts=None, max_q=None, max_k=None, window=0, sinks=0, stream=None):
+    """Either q, out [b, H_q, n_q, 128] and k, v [b, H_kv, n_k, 128] (any strides), or, with q_starts and k_starts (int32
+    [b + 1]), rows of sequences one after the other: q, out [rows, H_q, 128], k, v [rows, H_kv, 128] and max_q, max_k the longest
+    sequence's.  fp16 or bf16, all alike."""
+    _on_device(q, k, v, out, q_starts, k_starts)
+    p = kivi_prompt_t(head_dim=128, type=_type_of(q), window=window, sinks=sinks, softmax_scale=softmax_scale)
+    assert _type_of(k) == _type_of(v) == _type_of(out) == p.type, "q, k, v and out have one type"
+    assert out.shape == q.shape and v.shape == k.shape, "out is shaped like q, v like k"
+    if q_starts is not None:
+        assert k_starts is not None and q_starts.numel() == k_starts.numel() and max_q is not None and max_k is not None
+        p.batch, p.n_q_heads, p.n_kv_heads = q_starts.numel() - 1, q.shape[1], k.shape[1]
+        p.max_q, p.max_k, p.q_rows, p.k_rows = max_q, max_k, q.shape[0], k.shape[0]
+        p.q_starts, p.k_starts = _int32(q_starts), _int32(k_starts)
+        tensors = [_rows(x) for x in (q, k, v, out)]
+    else:
+        assert k_starts is None and q.dim() == 4 and q.shape[0] == k.shape[0] and q.shape[3] == k.shape[3] == 128
+        p.batch, p.n_q_heads, p.max_q = q.shape[:3]
+        p.n_kv_heads, p.max_k = k.shape[1:3]
+        tensors = [kivi_tensor_t(x.data_ptr(), *_strides_bht(x)) for x in (q, k, v, out)]
+    lib = load_library()
+    need = ctypes.c_size_t(0)
+    _check(lib.kivi_prompt_workspace_bytes(ctypes.byref(p), ctypes.byref(need)), "kivi_prompt_workspace_bytes")
+    workspace = None
+    if need.value:
+        import torch
+        workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+    handle = _stream_handle(stream)
+    if workspace is not None and stream is not None:
+        workspace.record_stream(stream)
+    _check(lib.kivi_prompt_attention(ctypes.byref(p), *(ctypes.byref(t) for t in tensors),
+                                     workspace.data_ptr() if workspace is not None else None, need.value, handle), "kivi_prompt_attention")
+    return out
+
+
+def make_paged_layout(max_sequences, n_q_heads, n_kv_heads, bits, residual, page_tokens, n_pages, cap_r_tokens, head_dim=128, group=32) -> kivi_paged_layout_t:
+    return kivi_paged_layout_t(max_sequences, n_q_heads, n_kv_heads, head_dim, bits, group, residual, page_tokens, n_pages, cap_r_tokens)
+
+
+def kivi_paged_sizes(layout: kivi_paged_layout_t) -> kivi_paged_sizes_t:
+    sizes = kivi_paged_sizes_t()
+    _check(load_library().kivi_paged_sizes(ctypes.byref(layout), ctypes.byref(sizes)), "kivi_paged_sizes")
+    return sizes
+
+
+class PagedCache:
+    """Device buffers of a paged cache (or the caller's own: contiguous CUDA tensors of at least those sizes) and the workspace of
+    its attention.  Calls of kivi_paged_attention that may overlap need a PagedCache each, over the same buffers."""
+
+    def __init__(self, layout: kivi_paged_layout_t, device="cuda", pages=None, k_resid=None, v_resid=None):
+        import torch
+        self.layout = layout
+        sizes = kivi_paged_sizes(layout)
+        self.c = kivi_paged_cache_t()
+        self.buffers = {}
+        for name, given in (("pages", pages), ("k_resid", k_resid), ("v_resid", v_resid)):
+            n = getattr(sizes, name)
+            if given is None:
+                given = torch.empty(n, dtype=torch.uint8, device=device)
+            assert given.is_cuda and given.is_contiguous() and given.numel() * given.element_size() >= n, f"{name}: {n} contiguous bytes"
+            self.buffers[name] = given
+            setattr(self.c, name, given.data_ptr())
+        self.workspace = torch.zeros(sizes.workspace, dtype=torch.uint8, device=self.buffers["pages"].device)
+
+    def records(self):
+        """The pages as int32 words [n_pages, H_kv, records per page, words of a record]."""
+        import torch
+        l = self.layout
+        return self.buffers["pages"].view(torch.uint8).flatten()[:kivi_paged_sizes(l).pages].view(torch.int32).view(
+            l.n_pages, l.n_kv_heads, l.page_tokens // 32, -1)
+
+    def rows(self, name):
+        """k_resid or v_resid as fp16 [max_sequences, H_kv, cap_r, 128]."""
+        import torch
+        l = self.layout
+        return self.buffers[name].view(torch.uint8).flatten()[:kivi_paged_sizes(l).k_resid].view(torch.float16).view(
+            l.max_sequences, l.n_kv_heads, l.cap_r_tokens, 128)
+
+
+class PagedBatch:
+    """The sequences of a call: page_table int32 [b, max_pages] (rows may be strided), lengths int32 [b], slots int32 [b] or None."""
+
+    def __init__(self, page_table, lengths, slots=None):
+        import torch
+        n = lengths.numel()
+        assert page_table.dim() == 2 and page_table.shape[0] == n and page_table.dtype == torch.int32 and (page_table.shape[1] < 2 or page_table.stride(1) == 1)
+        self.page_table, self.lengths, self.slots = page_table, lengths, slots
+        self.c = kivi_paged_batch_t(n, page_table.shape[1], max(page_table.stride(0), page_table.shape[1]), page_table.data_ptr(),
+                                    _int32(lengths), _int32(slots, n))
+
+
+def kivi_paged_append(cache: PagedCache, batch: PagedBatch, k, v, starts=None, max_new=1, rotation: Optional[Rotation] = None, positions=None,
+                      q=None, q_out=None, stream=None):
+    """k, v: CUDA fp16 / bf16 [rows, H_kv, 128] (any row and head strides), the new rows of all sequences: those of
+    sequence b are rows starts[b] .. starts[b + 1] - 1 (int32 [b + 1]), or max_new of each without starts.  batch.lengths counts them
+    already.  q [rows, H_q, 128] is rotated into q_out (fp16)."""
+    _on_device(k, v, starts, positions, q, q_out, batch.lengths, cache.workspace, rotation.table if rotation else None)
+    l, n = cache.layout, k.shape[0]
+    assert v.dtype == k.dtype and (q is None or q.dtype == k.dtype), "k, v and q have one type"
+    assert (q is None) == (q_out is None) and (q_out is None or _type_of(q_out) == KIVI_TYPE_FP16), "q goes into an fp16 q_out"
+    rows = kivi_paged_rows_t(k=_rows(k, l.n_kv_heads), v=_rows(v, l.n_kv_heads, n), type=_type_of(k), n_rows=n, max_new=max_new,
+                             starts=_int32(starts, batch.c.batch + 1))
+    if q is not None:
+        rows.q, rows.q_out = _rows(q, l.n_q_heads, n), _rows(q_out, l.n_q_heads, n)
+    if rotation is not None:
+        r = rotation.c(positions, n)
+        rows.rotation = ctypes.pointer(r)
+    _check(load_library().kivi_paged_append(ctypes.byref(l), ctypes.byref(cache.c), ctypes.byref(batch.c), ctypes.byref(rows),
+                                            _stream_handle(stream)), "kivi_paged_append")
+
+
+def kivi_paged_attention(cache: PagedCache, batch: PagedBatch, q_fp16, softmax_scale, out, window=0, sinks=0, stream=None):
+    """q_fp16: contiguous CUDA fp16 [b, H_q, 128]; out: the same shape, contiguous, fp16 or bf16."""
+    _on_device(q_fp16, out, batch.lengths, cache.workspace)
+    l = cache.layout
+    assert _type_of(q_fp16) == KIVI_TYPE_FP16 and q_fp16.is_contiguous() and out.is_contiguous()
+    assert tuple(q_fp16.shape) == tuple(out.shape) == (batch.c.batch, l.n_q_heads, 128), "q and out are [b, H_q, 128]"
+    query = kivi_paged_query_t(q_fp16.data_ptr(), out.data_ptr(), _type_of(out), window, sinks, softmax_scale)
+    _check(load_library().kivi_paged_attention(ctypes.byref(l), ctypes.byref(cache.c), ctypes.byref(batch.c), ctypes.byref(query),
+                                               cache.workspace.data_ptr(), cache.workspace.numel(), _stream_handle(stream)), "kivi_paged_attention")
+    return out
