@@ -52,6 +52,7 @@ constexpr float kNothing = -1e30f;     // running maximum of a row that has seen
 template <int CTRL>
 __device__ __forceinline__ float dpp(float x) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, true)); }
 constexpr int kRor8 = 0x128;           // the other column of a head
+constexpr int kRor4 = 0x124;
 template <int BANKS>                   // x of the other column in the lanes of BANKS, own in the others
 __device__ __forceinline__ half2v from_partner(half2v own, half2v x) {
     return __builtin_bit_cast(half2v, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, own), __builtin_bit_cast(int, x), kRor8, 0xF, BANKS, false));
@@ -107,6 +108,34 @@ __device__ __forceinline__ half8 value_fragment(const uint32_t* w, int pair, int
     return f.h;
 }
 
+__device__ __forceinline__ void wave_lds_sync() {      // LDS instructions of one wavefront execute in order
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");
+}
+// Workgroup barrier that orders LDS traffic only (a __syncthreads() would also wait for the copies in flight)
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+// Wave-uniform read of what earlier work left in memory, through the scalar cache
+__device__ __forceinline__ int scalar(const int32_t* base, int64_t i) {
+    return reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(base))[i];
+}
+// Asynchronous copy of 16 bytes per lane to LDS offset lds + 16 lane.  (Wait states between a vector instruction that writes the scalar operand and
+// this one: the compiler does not look into the block.  m0 is a reserved register, so the compiler warns that it keeps no value there: nor shall it.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void copy_to_lds(const void* base, uint32_t lane_offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(lds), "v"(lane_offset), "s"(base) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+template <int N>
+__device__ __forceinline__ void wait_copies() {        // at most N vector-memory operations still in flight
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
 struct Args : PagedAttentionParams {
     int32_t runs, run;                 // runs of query heads per kv-head, heads of a run
 };
@@ -141,17 +170,18 @@ __device__ __forceinline__ View view_of(const Args& p, int length, int slot) {
     v.steps = (v.records + kWaves - 1) / kWaves;
     return v;
 }
-__device__ __forceinline__ View view_of(const Args& p, int b) { return view_of(p, p.lengths[b], p.slots ? p.slots[b] : b); }
-
 template <int BITS, int HP>
-__global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(Args p) {
+__global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p) {
     constexpr int kCodeBytes = kTileTokens * kHeadDim * BITS / 8, kPlanes = BITS / 2, kScaleOff = kCodeBytes;
-    constexpr int kRecord = record_bytes(BITS);
+    constexpr int kRecord = record_bytes(BITS), NI = kRecord / 1024;   // copy instructions of a record
+    constexpr int NB = BITS == 2 ? 3 : 2;                              // records in flight per wavefront
     constexpr int NS = HP / 2;                                         // value-side operands: columns of a head share the channel groups
-    __shared__ __align__(16) unsigned char sm_record[kWaves][kRecord];
-    __shared__ __align__(16) float sm_o[kWaves][HP][kHeadDim];
+    constexpr int HR = BITS == 4 && HP == 8 ? 4 : HP;                  // heads that meet in LDS at once
+    __shared__ __align__(16) unsigned char sm_ring[kWaves][NB][kRecord];
+    __shared__ __align__(16) float sm_o[kWaves][HR][kHeadDim];
     __shared__ float sm_ml[kWaves][HP][2];
     __shared__ int sm_last;
+    static_assert(sizeof(sm_ring) + sizeof(sm_o) + sizeof(sm_ml) + 16 <= 160 * 1024 / 3 / 1280 * 1280, "three workgroups per compute unit");
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, kb = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool is_lo = n >= 8;
@@ -163,297 +193,459 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(Args p)
 
     // ---- this workgroup's interval of the axis ----
     const int wg = ((int)blockIdx.x & 7) * (kWorkgroups / 8) + ((int)blockIdx.x >> 3);      // neighbours on the axis share a die
-    int total = 0;
-    for (int b0 = 0; b0 < p.batch; b0 += 64) {
-        int c = b0 + lane < p.batch ? view_of(p, b0 + lane).cost() * units_per_sequence : 0;
+    auto cost_of = [&](int b) { return b < p.batch ? view_of(p, p.lengths[b], p.slots ? p.slots[b] : b).cost() * units_per_sequence : 0; };
+    auto sum_upto = [&](int x) {                                       // of this and the lanes before
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) c += __shfl_xor(c, d);
-        total += c;
-    }
+        for (int d = 1; d < 64; d <<= 1) {
+            const int y = __shfl_up(x, d);
+            if (lane >= d) x += y;
+        }
+        return x;
+    };
+    const int cost0 = cost_of(lane), upto0 = sum_upto(cost0);
+    int total = __shfl(upto0, 63);
+    for (int b0 = 64; b0 < p.batch; b0 += 64) total += __shfl(sum_upto(cost_of(b0 + lane)), 63);
+    total = __builtin_amdgcn_readfirstlane(total);
     const int length = max((total + kWorkgroups - 1) / kWorkgroups, kMinCost);
     const int x0 = wg * length, x1 = min(x0 + length, total);
     if (x0 >= x1) return;
     int b = 0, before = 0;                                             // the sequence of x0, and where it begins
-    {
-        int sum = 0;
-        for (int b0 = 0; b0 < p.batch; b0 += 64) {
-            const int mine = b0 + lane < p.batch ? view_of(p, b0 + lane).cost() * units_per_sequence : 0;
-            int upto = mine;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int x = __shfl_up(upto, d);
-                if (lane >= d) upto += x;
-            }
-            const uint64_t here = __ballot(sum + upto > x0);
-            if (here) {
-                const int at = __builtin_ctzll(here);
-                b = b0 + at;
-                before = sum + __shfl(upto - mine, at);
-                break;
-            }
-            sum += __shfl(upto, 63);
+    for (int b0 = 0, sum = 0; b0 < p.batch; b0 += 64) {
+        const int mine = b0 ? cost_of(b0 + lane) : cost0, upto = b0 ? sum_upto(mine) : upto0;
+        const uint64_t here = __ballot(sum + upto > x0);
+        if (here) {
+            const int at = __builtin_ctzll(here);
+            b = b0 + at;
+            before = sum + __shfl(upto - mine, at);
+            break;
         }
+        sum += __shfl(upto, 63);
     }
-    b = __builtin_amdgcn_readfirstlane(b);
+    // A place on the axis: sequence, unit in it, and where the unit begins
+    struct Place { int b, unit, unit0; View view; };
+    auto next_unit = [&](Place& u) {                                   // (only where another one follows)
+        u.unit0 += u.view.cost();
+        if (++u.unit == units_per_sequence) {
+            u.unit = 0;
+            do {
+                ++u.b;
+                u.view = view_of(p, scalar(p.lengths, u.b), p.slots ? scalar(p.slots, u.b) : u.b);
+            } while (u.view.cost() == 0);
+        }
+    };
+    // its steps of records in this interval: [first, end)
+    auto records_from = [&](const Place& u) { return max(x0 - u.unit0 - u.view.row_steps * kRowCost, 0); };
+    auto records_to = [&](const Place& u) { return max(min(x1 - u.unit0, u.view.cost()) - u.view.row_steps * kRowCost, 0); };
+    Place here;
+    here.b = __builtin_amdgcn_readfirstlane(b);
+    here.view = view_of(p, scalar(p.lengths, here.b), p.slots ? scalar(p.slots, here.b) : here.b);
     before = __builtin_amdgcn_readfirstlane(before);
-    View view = view_of(p, b);
-    int unit = (x0 - before) / view.cost();                            // of the sequence
+    here.unit = (x0 - before) / here.view.cost();
+    here.unit0 = before + here.unit * here.view.cost();
 
-    float4v acc[8], zsum, ro[8];
-    float m, l, prob_exp;
-    half2v qz[4][4], qk[4][4];
-    float c_zero, c_code;
-
-
-    int x = x0;
-    bool first_unit = true;
-    while (true) {
-        const int cost = view.cost(), unit0 = before + unit * cost;    // where the unit begins
-        const int kvh = unit / p.runs, h0 = (unit - kvh * p.runs) * p.run, live = min(p.run, rep - h0);
-        const int64_t q_row = (int64_t)b * p.n_q_heads + kvh * rep + h0;
-        const int slot = p.slots ? p.slots[b] : b;
-        const __half* k_ring = p.k_resid + ((int64_t)slot * p.n_kv_heads + kvh) * p.cap_r * kHeadDim;
-        const __half* v_ring = p.v_resid + ((int64_t)slot * p.n_kv_heads + kvh) * p.cap_r * kHeadDim;
-        // ---- query ----
-        {
-            Frag raw[4];
-            float mx = 0.f;
+    // ---- copies of records into this wavefront's ring, NB ahead ----
+    const uint32_t ring_lds = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)&sm_ring[wave][0][0]);
+    const uint32_t lane16 = lane * 16;
+    Place cursor = here;
+    int c_step = records_from(cursor), c_end = records_to(cursor), c_slot = 0, in_flight = 0;
+    uint32_t lost = 0;                                                 // slots whose record has no page
+    auto advance_copy = [&]() {
+        while (c_step >= c_end) {
+            if (cursor.unit0 + cursor.view.cost() >= x1) return;
+            next_unit(cursor);
+            c_step = 0;
+            c_end = records_to(cursor);
+        }
+        const int i = min(c_step * kWaves + wave, cursor.view.records - 1);     // (no record for this wavefront: any)
+        const int r = i < cursor.view.sink_records ? i : i + cursor.view.skip;
+        int page = scalar(p.page_table, cursor.b * p.page_table_stride + (r >> p.page_shift));
+        const bool bad = page < 0 || page >= p.n_pages;
+        lost = (lost & ~(1u << c_slot)) | (bad ? 1u << c_slot : 0u);
+        if (bad) page = 0;
+        const int kvh = cursor.unit / p.runs;
+        const char* rec = p.pages + (((((int64_t)page * p.n_kv_heads + kvh) << p.page_shift) + (r & ((1 << p.page_shift) - 1))) * kRecord);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");             // the slot's last readers have their data
 #pragma unroll
-            for (int cb = 0; cb < 4; ++cb) {
-                raw[cb].v = *reinterpret_cast<const uint4v*>(p.q + (q_row + min(head, live - 1)) * kHeadDim + cb * 32 + kb * 8);
+        for (int j = 0; j < NI; ++j) copy_to_lds(rec + j * 1024, lane16, ring_lds + c_slot * kRecord + j * 1024);
+        c_slot = c_slot + 1 == NB ? 0 : c_slot + 1;
+        ++c_step;
+        ++in_flight;
+    };
+    auto wait_oldest = [&]() {
+        if (in_flight >= NB) wait_copies<(NB - 1) * NI>();
+        else if (NB > 2 && in_flight == 2) wait_copies<NI>();
+        else wait_copies<0>();
+        --in_flight;
+    };
+
+    // ---- state of a wavefront ----
+    float4v acc[8];                    // code sums: acc[u][i] = channel 16 u + 4 kb + i, column n
+    float4v zsum;                      // zero-point sums: channel group i, column n
+    float m, l, prob_exp;              // running maximum (log2 domain), this lane's sum, exponent of the probabilities
+    half2v qz[4][4], qk[4][4];         // q 2^a; times 1 / place of the codes
+    half2v q_zero[4];                  // HP < 8: q 2^a of channel block n / 4
+    float c_code, c_zero;              // logit = code sum * c_code + zero sum * c_zero
+    half2v rounded[4] = {};            // keys' products in the lo columns, 0 in the hi columns
+    constexpr uint64_t kLoColumns = 0xFF00FF00FF00FF00ull;
+
+    auto set_query = [&](const half8 (&raw)[4]) {
+        float mx = 0.f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) mx = fmaxf(mx, fabsf((float)raw[cb].h[e]));
+        for (int cb = 0; cb < 4; ++cb)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) mx = fmaxf(mx, fabsf((float)raw[cb][e]));
+        mx = max_rows(mx);
+        const bool on = mx > 0.f;
+        const int a = on ? min(kQueryExp + 127 - (int)(__float_as_uint(mx) >> 23), 28) : 0, a1 = a / 2;
+        const _Float16 up1 = on ? (_Float16)__uint_as_float((uint32_t)(127 + a1) << 23) : (_Float16)0.f;
+        const _Float16 up2 = (_Float16)__uint_as_float((uint32_t)(127 + a - a1) << 23);
+        c_zero = p.softmax_scale * kLog2e * __uint_as_float((uint32_t)(127 - a) << 23);
+        c_code = c_zero * kKeyUnscale;
+#pragma unroll
+        for (int cb = 0; cb < 4; ++cb) {
+            Frag f;
+            f.h = raw[cb];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const _Float16 pf = BITS == 2 ? (_Float16)(1.f / (float)(1 << (2 * r))) : (_Float16)((r & 1) ? 1.f / 16.f : 1.f);
+                qz[cb][r] = f.p[r] * half2v{up1, up1} * half2v{up2, up2};
+                qk[cb][r] = qz[cb][r] * half2v{pf, pf};
             }
-            mx = max_rows(mx);
-            const bool on = mx > 0.f;
-            const int a = on ? min(kQueryExp + 127 - (int)(__float_as_uint(mx) >> 23), 28) : 0, a1 = a / 2;
-            const _Float16 up1 = on ? (_Float16)__uint_as_float((uint32_t)(127 + a1) << 23) : (_Float16)0.f;
-            const _Float16 up2 = (_Float16)__uint_as_float((uint32_t)(127 + a - a1) << 23);
-            c_zero = p.softmax_scale * kLog2e * __uint_as_float((uint32_t)(127 - a) << 23);
-            c_code = c_zero * kKeyUnscale;
+        }
+        if constexpr (HP < 8) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const half2v even = is_lo ? qz[2][r] : qz[0][r], odd = is_lo ? qz[3][r] : qz[1][r];
+                q_zero[r] = n & 4 ? odd : even;
+            }
+        }
+    };
+    auto query_frag = [&](int cb) -> half8 {
+        Frag f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) f.p[r] = qz[cb][r];
+        return f.h;
+    };
+    // Probabilities 2^(prob_exp + logit - m) of this lane's four tokens, logit = x cx + zk; raises the maximum, and rescales the state by
+    // rescale(factor), when a logit passes it by the slack
+    auto softmax = [&](const float (&x)[4], float cx, float zk, uint32_t live, float (&pv)[4], auto&& rescale) {
+        auto logits = [&](float off) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                pv[i] = fmaf(x[i], cx, off);
+                if (!((live >> i) & 1)) pv[i] = -INFINITY;
+                mx = fmaxf(mx, pv[i]);
+            }
+            return mx;
+        };
+        const float mx = logits(zk - (m - prob_exp));
+        if (__any(mx > prob_exp + kSlack)) {
+            float t = logits(zk);
+            t = max_rows(fmaxf(t, dpp<kRor8>(t)));
+            const float mn = fmaxf(m, t), f = __builtin_amdgcn_exp2f(m - mn);
+            rescale(f);
+            l *= f;
+            m = mn;
+            logits(zk - (m - prob_exp));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pv[i] = __builtin_amdgcn_exp2f(pv[i]);
+        l += (pv[0] + pv[1]) + (pv[2] + pv[3]);
+    };
+    auto rescale_acc = [&](float f) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) acc[u] *= f;
+        zsum *= f;
+    };
+    // fb: rounded (hi columns) or the remainder (lo columns), fa: the rounded ones in the lo columns, 0 in the others;
+    // lane kb gets tokens 8 kb .. 8 kb + 7
+    auto split = [&](const float (&pv)[4], Frag& fa, Frag& fb) {
+        const half2v none = {(_Float16)0.f, (_Float16)0.f};
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const half2v hi = pack_rtz(pv[2 * r], pv[2 * r + 1]);
+            float l0, l1;                              // the remainders (exact in fp32) with one mixed-precision instruction each
+            asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[0,0,0] op_sel_hi:[1,0,0]" : "=v"(l0) : "v"(hi), "v"(pv[2 * r]));
+            asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(l1) : "v"(hi), "v"(pv[2 * r + 1]));
+            const half2v lo = pack_rtz(l0, l1);
+            fb.p[r] = from_partner<kLoLanes>(hi, lo);
+            fb.p[r + 2] = from_partner<kHiLanes>(lo, hi);
+            fa.p[r] = from_partner<kLoLanes>(none, hi);
+            fa.p[r + 2] = is_lo ? hi : none;
+        }
+        auto exchange = [&](Frag& f) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                auto s = __builtin_amdgcn_permlane32_swap(f.r[r], f.r[r + 2], false, false);
+                f.r[r] = s[0];
+                f.r[r + 2] = s[1];
+            }
+        };
+        exchange(fa);
+        exchange(fb);
+    };
+    // which of this lane's tokens of a tile that begins with token t0 are visible
+    auto live_of = [&](const View& v, int t0) -> uint32_t {
+        uint32_t live = 0xF;
+        if (t0 < v.lowest || t0 + kTileTokens > v.length) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int t = t0 + tok + i;
+                if (t >= v.length || (t < v.lowest && t >= v.sinks)) live &= ~(1u << i);
+            }
+        }
+        return live;
+    };
+    auto any_above = [&](const unsigned char* scales, uint32_t limit) -> bool {      // of 128 scales, two per lane
+        typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
+        const uint32_t s2 = *reinterpret_cast<const uint32_t*>(scales + lane * 4), l2 = limit | limit << 16;
+        return __any(__builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, s2), __builtin_bit_cast(ushort2v, l2))) != l2);
+    };
+
+    // ---- one record out of an LDS slot ----
+    auto record_tile = [&](const unsigned char* sl, const View& v, int r) {
+        uint32_t w[2 * BITS];
+#pragma unroll
+        for (int pl = 0; pl < kPlanes; ++pl) {
+            const uint4v q4 = *reinterpret_cast<const uint4v*>(sl + pl * 1024 + (kb * 16 + row_pos) * 16);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[4 * pl + k] = q4[k];
+        }
+        const bool big = any_above(sl + kScaleOff, kKeyScaleLimit);
+        float4v d0 = {0.f, 0.f, 0.f, 0.f}, d1 = d0, dz = d0;
+        Frag s[4];
+#pragma unroll
+        for (int cb = 0; cb < 4; ++cb) {
+            s[cb].v = *reinterpret_cast<const uint4v*>(sl + kScaleOff + cb * 64 + kb * 16);
+            if constexpr (HP >= 8) {
+                Frag z;
+                z.v = *reinterpret_cast<const uint4v*>(sl + kScaleOff + 256 + cb * 64 + kb * 16);
+                dz = __builtin_amdgcn_mfma_f32_16x16x32_f16(z.h, query_frag(cb), dz, 0, 0, 0);
+            }
+        }
+        if constexpr (HP < 8) {
+            // (eight channels in each of the four columns that share a head and kb)
+            Frag z;
+            z.v = *reinterpret_cast<const uint4v*>(sl + kScaleOff + 256 + (n >> 2) * 64 + kb * 16);
+            float sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum = __builtin_amdgcn_fdot2(q_zero[k], z.p[k], sum, false);
+            sum += dpp<kRor8>(sum);
+            sum += dpp<kRor4>(sum);
+            dz[0] = add_rows(sum);
+        }
+        if (big) {
+            const half2v f = {(_Float16)(1.f / (1 << kKeyScaleShift)), (_Float16)(1.f / (1 << kKeyScaleShift))};
 #pragma unroll
             for (int cb = 0; cb < 4; ++cb)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const _Float16 pf = BITS == 2 ? (_Float16)(1.f / (float)(1 << (2 * r))) : (_Float16)((r & 1) ? 1.f / 16.f : 1.f);
-                    qz[cb][r] = raw[cb].p[r] * half2v{up1, up1} * half2v{up2, up2};
-                    qk[cb][r] = qz[cb][r] * half2v{pf, pf};
-                }
+                for (int k = 0; k < 4; ++k) s[cb].p[k] *= f;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            acc[i] = float4v{0.f, 0.f, 0.f, 0.f};
-            ro[i] = float4v{0.f, 0.f, 0.f, 0.f};
+        for (int cb = 0; cb < 4; ++cb) {
+            Frag f;
+            // in the lo columns alone; the hi columns' zeros stay
+            uint64_t active;
+            asm("s_and_saveexec_b64 %4, %13\n\tv_pk_mul_f16 %0, %5, %9\n\tv_pk_mul_f16 %1, %6, %10\n\tv_pk_mul_f16 %2, %7, %11\n\tv_pk_mul_f16 %3, %8, %12\n\ts_mov_b64 exec, %4"
+                : "+&v"(rounded[0]), "+&v"(rounded[1]), "+&v"(rounded[2]), "+&v"(rounded[3]), "=&s"(active)
+                : "v"(qk[cb][0]), "v"(qk[cb][1]), "v"(qk[cb][2]), "v"(qk[cb][3]), "v"(s[cb].p[0]), "v"(s[cb].p[1]), "v"(s[cb].p[2]), "v"(s[cb].p[3]), "s"(kLoColumns)
+                : "scc");
+#pragma unroll
+            for (int k = 0; k < 4; ++k) f.p[k] = __builtin_elementwise_fma(qk[cb][k], s[cb].p[k], -rounded[k]);
+            d0 = __builtin_amdgcn_mfma_f32_16x16x32_f16(key_fragment<BITS>(w, cb, 0), f.h, d0, 0, 0, 0);
+            d1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(key_fragment<BITS>(w, cb, 1), f.h, d1, 0, 0, 0);
         }
+        float x[4], pv[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            // hi and lo column of a head share its tokens: hi columns take tok0 + k, lo columns 16 + tok0 + k
+            x[k] = is_lo ? d1[k] : d0[k];
+            x[k] += dpp<kRor8>(is_lo ? d0[k] : d1[k]);
+        }
+        if (prob_exp > 0.f && any_above(sl + kScaleOff + 512, kValueScaleLimit<BITS>)) {
+            const float f = __builtin_amdgcn_exp2f(-(float)kSlack - prob_exp);
+            rescale_acc(f);
+            l *= f;
+            prob_exp = -(float)kSlack;
+        }
+        softmax(x, big ? c_code * (float)(1 << kKeyScaleShift) : c_code, dz[0] * c_zero, live_of(v, r * kTileTokens), pv, rescale_acc);
+        // outputs: this lane's tokens 8 kb .. 8 kb + 7, as pairs, of a channel group
+        Frag fa, fb, z;
+        split(pv, fa, fb);
+        const unsigned char* vs = sl + kScaleOff + 512 + kb * 64;
+        {
+            const uint32_t sel = (n & 1) ? 0x07060302u : 0x05040100u;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t t0 = *reinterpret_cast<const uint32_t*>(vs + 256 + 16 * k + (n & 2) * 2), t1 = *reinterpret_cast<const uint32_t*>(vs + 256 + 16 * k + 8 + (n & 2) * 2);
+                z.r[k] = __builtin_amdgcn_perm(t1, t0, sel);
+            }
+        }
+        zsum = __builtin_amdgcn_mfma_f32_16x16x32_f16(z.h, fb.h, zsum, 0, 0, 0);       // rows = channel groups
+        Frag sv[NS];
+        if constexpr (HP == 2) {
+            const uint32_t sel = (my_group & 1) ? 0x07060302u : 0x05040100u;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t t0 = *reinterpret_cast<const uint32_t*>(vs + 16 * k + (my_group & 2) * 2), t1 = *reinterpret_cast<const uint32_t*>(vs + 16 * k + 8 + (my_group & 2) * 2);
+                sv[0].r[k] = __builtin_amdgcn_perm(t1, t0, sel);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint4v t = *reinterpret_cast<const uint4v*>(vs + 16 * k);         // tokens 2 k and 2 k + 1, four groups each
+                if constexpr (HP == 4) {
+                    const uint32_t sel = my_group ? 0x07060302u : 0x05040100u;
+                    sv[0].r[k] = __builtin_amdgcn_perm(t[2], t[0], sel);
+                    sv[1].r[k] = __builtin_amdgcn_perm(t[3], t[1], sel);
+                } else {
+                    sv[0].r[k] = __builtin_amdgcn_perm(t[2], t[0], 0x05040100u);
+                    sv[1].r[k] = __builtin_amdgcn_perm(t[2], t[0], 0x07060302u);
+                    sv[2].r[k] = __builtin_amdgcn_perm(t[3], t[1], 0x05040100u);
+                    sv[3].r[k] = __builtin_amdgcn_perm(t[3], t[1], 0x07060302u);
+                }
+            }
+        }
+#pragma unroll
+        for (int pl = 0; pl < kPlanes; ++pl) {
+            const uint4v q4 = *reinterpret_cast<const uint4v*>(sl + kScaleOff + 1024 + pl * 1024 + lane16);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[4 * pl + k] = q4[k];
+        }
+        if constexpr (BITS == 2) {
+            const half2v pf = {(_Float16)0.25f, (_Float16)0.25f};
+            fa.p[1] *= pf; fa.p[3] *= pf;
+            fb.p[1] *= pf; fb.p[3] *= pf;
+        }
+        Frag f[NS];
+#pragma unroll
+        for (int g = 0; g < NS; ++g)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const half2v t = fa.p[k] * sv[g].p[k];
+                f[g].p[k] = __builtin_elementwise_fma(fb.p[k], sv[g].p[k], __builtin_elementwise_fma(fa.p[k], sv[g].p[k], -t));
+            }
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value_fragment<BITS>(w, u >> 1, u & 1), f[(u >> 1) * NS / 4].h, acc[u], 0, 0, 0);
+    };
+
+    // ---- 32 fp16 rows: keys are operands as they are; value rows, eight tokens by eight channels per lane, are turned in registers ----
+    auto row_tile = [&](const View& v, int64_t ring, int i, float4v (&ro)[8]) {
+        const int t0 = v.row0 + i * kTileTokens, last = v.length - 1, base = t0 % p.cap_r;
+        auto slot_of = [&](int t) {                                    // (rows past the end re-read the last one)
+            const int s = base + min(t, last) - t0;
+            return s >= p.cap_r ? s - p.cap_r : s;
+        };
+        Frag kr[2][4], vr[8];
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+            for (int cb = 0; cb < 4; ++cb)
+                kr[hf][cb].v = *reinterpret_cast<const uint4v*>(p.k_resid + ring + slot_of(t0 + hf * 16 + row_pos) * kHeadDim + cb * 32 + kb * 8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vr[e].v = *reinterpret_cast<const uint4v*>(p.v_resid + ring + slot_of(t0 + kb * 8 + e) * kHeadDim + n * 8);
+        float4v d[2];
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+            d[hf] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int cb = 0; cb < 4; ++cb) d[hf] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kr[hf][cb].h, query_frag(cb), d[hf], 0, 0, 0);
+        }
+        float x[4], pv[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = is_lo ? d[1][k] : d[0][k];
+        softmax(x, c_zero, 0.f, live_of(v, t0), pv, [&](float f) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ro[e] *= f;
+        });
+        Frag fa, fb;
+        split(pv, fa, fb);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            Frag a;                                                    // rows: channels 8 n + e
+#pragma unroll
+            for (int k = 0; k < 4; ++k) a.r[k] = __builtin_amdgcn_perm(vr[2 * k + 1].r[e / 2], vr[2 * k].r[e / 2], e & 1 ? 0x07060302u : 0x05040100u);
+            ro[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.h, fb.h, ro[e], 0, 0, 0);
+        }
+    };
+    // the lane of a head's pair of columns that holds channels 16 u + 4 kb .. of it
+    auto holds = [&](int u) { return !is_lo && (HP == 8 || (HP == 4 ? my_group == ((u >> 1) & 1) : my_group == (u >> 1))); };
+
+    bool first_unit = true;
+    int slot = 0;
+    advance_copy();
+    while (true) {
+        const View& view = here.view;
+        const int cost = view.cost(), kvh = here.unit / p.runs, h0 = (here.unit - kvh * p.runs) * p.run, live = min(p.run, rep - h0);
+        const int64_t q_row = (int64_t)here.b * p.n_q_heads + kvh * rep + h0;
+        {
+            Frag raw[4];
+            half8 r8[4];
+#pragma unroll
+            for (int cb = 0; cb < 4; ++cb) {
+                raw[cb].v = *reinterpret_cast<const uint4v*>(p.q + (q_row + min(head, live - 1)) * kHeadDim + cb * 32 + kb * 8);
+                r8[cb] = raw[cb].h;
+            }
+            set_query(r8);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) acc[u] = float4v{0.f, 0.f, 0.f, 0.f};
         zsum = float4v{0.f, 0.f, 0.f, 0.f};
         m = kNothing;
         l = 0.f;
         prob_exp = (float)kProbExp<BITS>;
-
-        auto rescale = [&](float f) {
+#pragma unroll 1
+        while (in_flight < NB) {
+            const int was = in_flight;
+            advance_copy();
+            if (in_flight == was) break;
+        }
+        // steps of fp16 rows that begin in the interval
+        const int rows_cost = view.row_steps * kRowCost, row_end = min(x1 - here.unit0, rows_cost);
+        const int row_from = (min(max(x0 - here.unit0, 0), rows_cost) + kRowCost - 1) / kRowCost;
+        if (row_from * kRowCost < row_end) {
+            const int slot_of_rows = p.slots ? scalar(p.slots, here.b) : here.b;
+            const int64_t ring = ((int64_t)slot_of_rows * p.n_kv_heads + kvh) * p.cap_r * kHeadDim;
+            float4v ro[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { acc[i] *= f; ro[i] *= f; }
-            zsum *= f;
-            l *= f;
-        };
-        // probabilities 2^(prob_exp + logit - m) of this lane's four tokens out of x[i] (log2 domain; -inf: masked)
-        auto softmax = [&](float (&x4)[4]) {
-            float mx = fmaxf(fmaxf(x4[0], x4[1]), fmaxf(x4[2], x4[3]));
-            if (__any(mx > m + kSlack || (m == kNothing && mx > kNothing))) {
-                mx = max_rows(fmaxf(mx, dpp<kRor8>(mx)));
-                const float mn = fmaxf(m, mx);
-                rescale(__builtin_amdgcn_exp2f(m - mn));
-                m = mn;
-            }
+            for (int e = 0; e < 8; ++e) ro[e] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int j = row_from; j * kRowCost < row_end; ++j)
+                if (j * kWaves + wave < view.row_tiles) row_tile(view, ring, j * kWaves + wave, ro);
+            // into the records' order
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x4[i] = __builtin_amdgcn_exp2f(x4[i] - m + prob_exp);
-            l += (x4[0] + x4[1]) + (x4[2] + x4[3]);
-        };
-        // fb: rounded (hi columns) or the remainder (lo columns), fa: the rounded ones in the lo columns, 0 in the others;
-        // lane kb gets tokens 8 kb .. 8 kb + 7
-        auto split = [&](const float (&pv)[4], Frag& fa, Frag& fb) {
-            const half2v none = {(_Float16)0.f, (_Float16)0.f};
+            for (int e = 0; e < 8; ++e)
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const half2v hi = pack_rtz(pv[2 * r], pv[2 * r + 1]);
-                const half2v lo = pack_rtz(pv[2 * r] - (float)hi[0], pv[2 * r + 1] - (float)hi[1]);
-                fb.p[r] = from_partner<kLoLanes>(hi, lo);
-                fb.p[r + 2] = from_partner<kHiLanes>(lo, hi);
-                fa.p[r] = from_partner<kLoLanes>(none, hi);
-                fa.p[r + 2] = is_lo ? hi : none;
-            }
-            auto exchange = [&](Frag& f) {
+                for (int i = 0; i < 4; ++i) ro[e][i] = (ro[e][i] + dpp<kRor8>(ro[e][i])) * (1.f / kValueUnscale);
+#pragma unroll 1
+            for (int g0 = 0; g0 < HP; g0 += HR) {
+                wave_lds_sync();
+                if (n >= g0 && n < g0 + HR) {
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    auto s = __builtin_amdgcn_permlane32_swap(f.r[r], f.r[r + 2], false, false);
-                    f.r[r] = s[0];
-                    f.r[r + 2] = s[1];
+                    for (int i = 0; i < 4; ++i) {
+                        float4v* dst = reinterpret_cast<float4v*>(&sm_o[wave][n - g0][(kb * 4 + i) * 8]);
+                        dst[0] = float4v{ro[0][i], ro[1][i], ro[2][i], ro[3][i]};
+                        dst[1] = float4v{ro[4][i], ro[5][i], ro[6][i], ro[7][i]};
+                    }
                 }
-            };
-            exchange(fa);
-            exchange(fb);
-        };
-        // mask of this lane's tokens of a tile that begins with token t0
-        auto mask = [&](int t0, float (&x4)[4]) {
-            if (t0 < view.lowest || t0 + kTileTokens > view.length) {
+                wave_lds_sync();
+                if (head >= g0 && head < g0 + HR) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int t = t0 + tok + i;
-                    if (t >= view.length || (t < view.lowest && t >= view.sinks)) x4[i] = -INFINITY;
+                    for (int u = 0; u < 8; ++u)
+                        if (holds(u)) acc[u] = *reinterpret_cast<const float4v*>(&sm_o[wave][head - g0][u * 16 + kb * 4]);
                 }
             }
-        };
-
-        auto record_tile = [&](int i) {
-            const int r = i < view.sink_records ? i : i + view.skip;
-            const int page = p.page_table[b * p.page_table_stride + (r >> p.page_shift)];
-            if (page < 0 || page >= p.n_pages) return;
-            const char* rec = p.pages + (((((int64_t)page * p.n_kv_heads + kvh) << p.page_shift) + (r & ((1 << p.page_shift) - 1))) * kRecord);
-            unsigned char* sl = &sm_record[wave][0];
-            uint4v in[kRecord / 1024];
-#pragma unroll
-            for (int j = 0; j < kRecord / 1024; ++j) in[j] = *reinterpret_cast<const uint4v*>(rec + j * 1024 + lane * 16);
-            __builtin_amdgcn_wave_barrier();
-#pragma unroll
-            for (int j = 0; j < kRecord / 1024; ++j) *reinterpret_cast<uint4v*>(sl + j * 1024 + lane * 16) = in[j];
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            uint32_t w[2 * BITS];
-#pragma unroll
-            for (int pl = 0; pl < kPlanes; ++pl) {
-                const uint4v v = *reinterpret_cast<const uint4v*>(sl + pl * 1024 + (kb * 16 + row_pos) * 16);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) w[4 * pl + k] = v[k];
-            }
-            // logits
-            const uint32_t ks2 = *reinterpret_cast<const uint32_t*>(sl + kScaleOff + lane * 4);
-            const bool big = __any(ks2 >> 16 >= kKeyScaleLimit || (ks2 & 0xFFFFu) >= kKeyScaleLimit);
-            float4v d0 = {0.f, 0.f, 0.f, 0.f}, d1 = d0, dz = d0;
-#pragma unroll
-            for (int cb = 0; cb < 4; ++cb) {
-                Frag s, z, f, qf;
-                s.v = *reinterpret_cast<const uint4v*>(sl + kScaleOff + cb * 64 + kb * 16);
-                z.v = *reinterpret_cast<const uint4v*>(sl + kScaleOff + 256 + cb * 64 + kb * 16);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (big) s.p[k] *= half2v{(_Float16)(1.f / (1 << kKeyScaleShift)), (_Float16)(1.f / (1 << kKeyScaleShift))};
-                    const half2v t = qk[cb][k] * s.p[k], none = {(_Float16)0.f, (_Float16)0.f};
-                    f.p[k] = __builtin_elementwise_fma(qk[cb][k], s.p[k], is_lo ? -t : none);
-                    qf.p[k] = qz[cb][k];
-                }
-                dz = __builtin_amdgcn_mfma_f32_16x16x32_f16(z.h, qf.h, dz, 0, 0, 0);
-                d0 = __builtin_amdgcn_mfma_f32_16x16x32_f16(key_fragment<BITS>(w, cb, 0), f.h, d0, 0, 0, 0);
-                d1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(key_fragment<BITS>(w, cb, 1), f.h, d1, 0, 0, 0);
-            }
-            float x4[4];
-            const float cx = big ? c_code * (float)(1 << kKeyScaleShift) : c_code, zk = dz[0] * c_zero;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                // hi and lo column of a head share its tokens: hi columns take tok0 + k, lo columns 16 + tok0 + k
-                x4[k] = is_lo ? d1[k] : d0[k];
-                x4[k] += dpp<kRor8>(is_lo ? d0[k] : d1[k]);
-                x4[k] = fmaf(x4[k], cx, zk);
-            }
-            mask(r * kTileTokens, x4);
-            // outputs
-            const uint32_t vs2 = *reinterpret_cast<const uint32_t*>(sl + kScaleOff + 512 + lane * 4);
-            if (prob_exp > 0.f && __any(vs2 >> 16 >= kValueScaleLimit<BITS> || (vs2 & 0xFFFFu) >= kValueScaleLimit<BITS>)) {
-                rescale(__builtin_amdgcn_exp2f(-(float)kSlack - prob_exp));
-                prob_exp = -(float)kSlack;
-            }
-            softmax(x4);
-            Frag fa, fb, z;
-            split(x4, fa, fb);
-            auto pairs = [&](int off, int group, Frag& to) {           // of this lane's tokens, one channel group
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint32_t a = *reinterpret_cast<const uint16_t*>(sl + off + (kb * 8 + 2 * k) * 8 + group * 2);
-                    const uint32_t c = *reinterpret_cast<const uint16_t*>(sl + off + (kb * 8 + 2 * k + 1) * 8 + group * 2);
-                    to.r[k] = a | c << 16;
-                }
-            };
-            pairs(kScaleOff + 768, n & 3, z);
-            zsum = __builtin_amdgcn_mfma_f32_16x16x32_f16(z.h, fb.h, zsum, 0, 0, 0);       // rows = channel groups
-            if constexpr (BITS == 2) {
-                const half2v pf = {(_Float16)0.25f, (_Float16)0.25f};
-                fa.p[1] *= pf; fa.p[3] *= pf;
-                fb.p[1] *= pf; fb.p[3] *= pf;
-            }
-            Frag f[NS];
-#pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                Frag sv;
-                pairs(kScaleOff + 512, HP == 2 ? my_group : HP == 4 ? 2 * s + my_group : s, sv);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const half2v t = fa.p[k] * sv.p[k];
-                    f[s].p[k] = __builtin_elementwise_fma(fb.p[k], sv.p[k], __builtin_elementwise_fma(fa.p[k], sv.p[k], -t));
-                }
-            }
-#pragma unroll
-            for (int pl = 0; pl < kPlanes; ++pl) {
-                const uint4v v = *reinterpret_cast<const uint4v*>(sl + kScaleOff + 1024 + pl * 1024 + lane * 16);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) w[4 * pl + k] = v[k];
-            }
-#pragma unroll
-            for (int u = 0; u < 8; ++u)
-                acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value_fragment<BITS>(w, u >> 1, u & 1), f[(u >> 1) * NS / 4].h, acc[u], 0, 0, 0);
-            __builtin_amdgcn_wave_barrier();
-        };
-        // 32 fp16 rows: keys are operands as they are; value rows, eight tokens by eight channels per lane, are turned in registers
-        auto row_tile = [&](int i) {
-            const int t0 = view.row0 + i * kTileTokens, last = view.length - 1;
-            const int base = t0 % p.cap_r;
-            auto slot_of = [&](int t) {                                // (rows past the end re-read the last one)
-                const int s = base + min(t, last) - t0;
-                return s >= p.cap_r ? s - p.cap_r : s;
-            };
-            Frag kr[2][4], vr[8];
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-                for (int cb = 0; cb < 4; ++cb)
-                    kr[hf][cb].v = *reinterpret_cast<const uint4v*>(k_ring + slot_of(t0 + hf * 16 + row_pos) * kHeadDim + cb * 32 + kb * 8);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) vr[e].v = *reinterpret_cast<const uint4v*>(v_ring + slot_of(t0 + kb * 8 + e) * kHeadDim + n * 8);
-            float4v d[2];
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-                d[hf] = float4v{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int cb = 0; cb < 4; ++cb) {
-                    Frag qf;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) qf.p[k] = qz[cb][k];
-                    d[hf] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kr[hf][cb].h, qf.h, d[hf], 0, 0, 0);
-                }
-            }
-            float x4[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) x4[k] = (is_lo ? d[1][k] : d[0][k]) * c_zero;
-            mask(t0, x4);
-            softmax(x4);
-            Frag fa, fb;
-            split(x4, fa, fb);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                Frag a;                                                // rows: channels 8 n + e
-#pragma unroll
-                for (int k = 0; k < 4; ++k) a.r[k] = __builtin_amdgcn_perm(vr[2 * k + 1].r[e / 2], vr[2 * k].r[e / 2], e & 1 ? 0x07060302u : 0x05040100u);
-                ro[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.h, fb.h, ro[e], 0, 0, 0);
-            }
-        };
-
-        // ---- the interval's steps of this unit ----
-        const int end = min(x1, unit0 + cost);
-        {
-            const int a = x - unit0, z = end - unit0;                  // steps that begin in [a, z)
-            const int rows_cost = view.row_steps * kRowCost;
-            for (int j = (min(a, rows_cost) + kRowCost - 1) / kRowCost; j * kRowCost < min(z, rows_cost); ++j)
-                if (j * kWaves + wave < view.row_tiles) row_tile(j * kWaves + wave);
-            for (int j = max(a - rows_cost, 0); j < z - rows_cost; ++j)
-                if (j * kWaves + wave < view.records) record_tile(j * kWaves + wave);
+            wave_lds_sync();
+        }
+        const int j1 = records_to(here);
+        for (int j = records_from(here); j < j1; ++j) {
+            wait_oldest();
+            const int i = j * kWaves + wave;
+            if (i < view.records && !((lost >> slot) & 1)) record_tile(&sm_ring[wave][slot][0], view, i < view.sink_records ? i : i + view.skip);
+            advance_copy();
+            slot = slot + 1 == NB ? 0 : slot + 1;
         }
         // ---- leave the unit ----
         {
@@ -462,36 +654,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(Args p)
                 sm_ml[wave][lane][0] = m - prob_exp;                   // sums and outputs are relative to 2^this
                 sm_ml[wave][lane][1] = lw;
             }
-            // outputs of the records: head `head`, channels 16 u + 4 kb + i; of the rows: channels 8 (4 kb + i) + e
-            float zz[4];
-#pragma unroll
-            for (int g = 0; g < 4; ++g) zz[g] = zsum[g] + dpp<kRor8>(zsum[g]);
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int g = u >> 1;
-                float4v o;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = fmaf(acc[u][i] + dpp<kRor8>(acc[u][i]), kValueUnscale, zz[g]);
-                const bool valid = !is_lo && (HP == 8 || (HP == 4 ? my_group == (g & 1) : my_group == g));
-                if (valid) *reinterpret_cast<float4v*>(&sm_o[wave][head][u * 16 + kb * 4]) = o;
-            }
-            __builtin_amdgcn_wave_barrier();
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) ro[e][i] += dpp<kRor8>(ro[e][i]);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            if (n < HP) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float4v* dst = reinterpret_cast<float4v*>(&sm_o[wave][n][(kb * 4 + i) * 8]);
-                    dst[0] += float4v{ro[0][i], ro[1][i], ro[2][i], ro[3][i]};
-                    dst[1] += float4v{ro[4][i], ro[5][i], ro[6][i], ro[7][i]};
-                }
-            }
         }
-        __syncthreads();
-        const int owner0 = unit0 / length, parts = (unit0 + cost - 1) / length - owner0 + 1;
+        const int owner0 = here.unit0 / length, parts = (here.unit0 + cost - 1) / length - owner0 + 1;
         auto write_out = [&](int hh, int c, float ox, float oy, float sum) {
             const float f = sum > 0.f ? 1.f / sum : 0.f;
             const int64_t i = (q_row + hh) * kHeadDim + c;
@@ -502,62 +666,88 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(Args p)
                 *reinterpret_cast<half2v*>(static_cast<_Float16*>(p.out) + i) = half2v{(_Float16)(ox * f), (_Float16)(oy * f)};
             }
         };
-        const int c2 = (tid & 63) * 2;
-        const int my_part = wg * 2 + (first_unit ? 0 : 1);
-        for (int hh = wave; hh < live; hh += kWaves) {
-            float mm = kNothing, sum = 0.f, ox = 0.f, oy = 0.f;
+        const int c2 = (tid & 63) * 2, my_part = wg * 2 + (first_unit ? 0 : 1);
+        float zz[4];
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, sm_ml[w][hh][0]);
+        for (int g = 0; g < 4; ++g) zz[g] = zsum[g] + dpp<kRor8>(zsum[g]);
+#pragma unroll 1
+        for (int g0 = 0; g0 < HP; g0 += HR) {
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                const float f = __builtin_amdgcn_exp2f(sm_ml[w][hh][0] - mm);
-                sum = fmaf(sm_ml[w][hh][1], f, sum);
-                ox = fmaf(sm_o[w][hh][c2], f, ox);
-                oy = fmaf(sm_o[w][hh][c2 + 1], f, oy);
+            for (int u = 0; u < 8; ++u) {
+                float4v o;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = fmaf(acc[u][i] + dpp<kRor8>(acc[u][i]), kValueUnscale, zz[u >> 1]);
+                if (holds(u) && head >= g0 && head < g0 + HR) *reinterpret_cast<float4v*>(&sm_o[wave][head - g0][u * 16 + kb * 4]) = o;
             }
-            if (parts == 1) {
-                write_out(hh, c2, ox, oy, sum);
-            } else {
-                store_shared(p.part_o + ((int64_t)my_part * kMaxHeads + hh) * kPartFloats + c2, ox, oy);
-                if (lane == 0) store_shared(p.part_ml + ((int64_t)my_part * kMaxHeads + hh) * 2, mm, sum);
+            lds_barrier();
+            for (int hh = g0 + wave; hh < min(g0 + HR, live); hh += kWaves) {
+                float mm = kNothing, sum = 0.f, ox = 0.f, oy = 0.f;
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, sm_ml[w][hh][0]);
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) {
+                    const float f = __builtin_amdgcn_exp2f(sm_ml[w][hh][0] - mm);
+                    const float2 o2 = *reinterpret_cast<const float2*>(&sm_o[w][hh - g0][c2]);
+                    sum = fmaf(sm_ml[w][hh][1], f, sum);
+                    ox = fmaf(o2.x, f, ox);
+                    oy = fmaf(o2.y, f, oy);
+                }
+                if (parts == 1) {
+                    write_out(hh, c2, ox, oy, sum);
+                } else {
+                    store_shared(p.part_o + ((int64_t)my_part * kMaxHeads + hh) * kPartFloats + c2, ox, oy);
+                    if (lane == 0) store_shared(p.part_ml + ((int64_t)my_part * kMaxHeads + hh) * 2, mm, sum);
+                }
             }
+            lds_barrier();                                             // (LDS is written again)
         }
         if (parts > 1) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // the part is where the others can see it
+            lds_barrier();
             if (tid == 0) sm_last = __hip_atomic_fetch_add(p.counters + owner0, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
-            __syncthreads();
+            lds_barrier();
             if (sm_last) {
+                // the unit is the first one of every workgroup but, maybe, the first of them
+                const int second = owner0 * length < here.unit0 ? 1 : 0;
+                constexpr int kBatch = 8;
                 for (int hh = wave; hh < live; hh += kWaves) {
                     float mm = kNothing, sum = 0.f, ox = 0.f, oy = 0.f;
-                    for (int g = 0; g < parts; ++g) {
-                        // the unit is the first one of every workgroup but, maybe, the first of them
-                        const int part = (owner0 + g) * 2 + (g == 0 && owner0 * length < unit0 ? 1 : 0);
-                        const float2 st = load_shared(p.part_ml + ((int64_t)part * kMaxHeads + hh) * 2);
-                        const float2 o2 = load_shared(p.part_o + ((int64_t)part * kMaxHeads + hh) * kPartFloats + c2);
-                        const float mn = fmaxf(mm, st.x), f0 = __builtin_amdgcn_exp2f(mm - mn), f1 = __builtin_amdgcn_exp2f(st.x - mn);
+#pragma unroll 1
+                    for (int g0 = 0; g0 < parts; g0 += kBatch) {
+                        float2 st[kBatch], o2[kBatch];
+#pragma unroll
+                        for (int g = 0; g < kBatch; ++g) {
+                            const int at = min(g0 + g, parts - 1), part = (owner0 + at) * 2 + (at == 0 ? second : 0);
+                            st[g] = load_shared(p.part_ml + ((int64_t)part * kMaxHeads + hh) * 2);
+                            o2[g] = load_shared(p.part_o + ((int64_t)part * kMaxHeads + hh) * kPartFloats + c2);
+                        }
+                        float mn = mm;
+#pragma unroll
+                        for (int g = 0; g < kBatch; ++g) mn = fmaxf(mn, st[g].x);
+                        const float f0 = __builtin_amdgcn_exp2f(mm - mn);
                         mm = mn;
-                        sum = fmaf(st.y, f1, sum * f0);
-                        ox = fmaf(o2.x, f1, ox * f0);
-                        oy = fmaf(o2.y, f1, oy * f0);
+                        sum *= f0;
+                        ox *= f0;
+                        oy *= f0;
+#pragma unroll
+                        for (int g = 0; g < kBatch; ++g) {
+                            const float f = g0 + g < parts ? __builtin_amdgcn_exp2f(st[g].x - mn) : 0.f;
+                            sum = fmaf(st[g].y, f, sum);
+                            ox = fmaf(o2[g].x, f, ox);
+                            oy = fmaf(o2[g].y, f, oy);
+                        }
                     }
                     write_out(hh, c2, ox, oy, sum);
                 }
                 if (tid == 0) __hip_atomic_store(p.counters + owner0, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
+            lds_barrier();
         }
-        if (end >= x1) break;
-        __syncthreads();
-        x = end;
+        if (here.unit0 + cost >= x1) break;
         first_unit = false;
-        if (++unit == units_per_sequence) {
-            before += units_per_sequence * cost;
-            unit = 0;
-            do {
-                view = view_of(p, ++b);
-            } while (view.cost() == 0);                                // (x < total: there is another sequence with tokens)
-        }
+        next_unit(here);
     }
+    wait_copies<0>();                                                  // no copy may land in LDS that has been given back
 }
 
 }  // namespace
