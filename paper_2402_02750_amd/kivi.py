@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 _PKG_DIR = os.path.dirname(os.path.abspath(__file__))
@@ -160,13 +161,13 @@ def load_library() -> ctypes.CDLL:
                                             ctypes.c_float, I32, VP, VP, ctypes.c_size_t, VP]
     lib.kivi_decode_attention_ragged.argtypes = [P(kivi_layout_t), P(kivi_cache_t), P(kivi_seq_state_t), VP,
                                                  ctypes.c_float, VP, VP, ctypes.c_size_t, VP]
-    lib.kivi_norm_rotate.argtypes = [P(kivi_norm_rotate_job_t), I32, I32, ctypes.c_float, P(kivi_rotation_t), VP]
-    lib.kivi_prompt_workspace_bytes.argtypes = [P(kivi_prompt_t), P(ctypes.c_size_t)]
-    lib.kivi_prompt_attention.argtypes = [P(kivi_prompt_t)] + [P(kivi_tensor_t)] * 4 + [VP, ctypes.c_size_t, VP]
-    lib.kivi_paged_sizes.argtypes = [P(kivi_paged_layout_t), P(kivi_paged_sizes_t)]
-    lib.kivi_paged_append.argtypes = [P(kivi_paged_layout_t), P(kivi_paged_cache_t), P(kivi_paged_batch_t), P(kivi_paged_rows_t), VP]
-    lib.kivi_paged_attention.argtypes = [P(kivi_paged_layout_t), P(kivi_paged_cache_t), P(kivi_paged_batch_t), P(kivi_paged_query_t),
-                                         VP, ctypes.c_size_t, VP]
+    # (structs by address: byref() of one above, or the same fields packed into bytes, which takes a third of the time)
+    lib.kivi_norm_rotate.argtypes = [VP, I32, I32, ctypes.c_float, VP, VP]
+    lib.kivi_prompt_workspace_bytes.argtypes = [VP, VP]
+    lib.kivi_prompt_attention.argtypes = [VP] * 6 + [ctypes.c_size_t, VP]
+    lib.kivi_paged_sizes.argtypes = [VP, VP]
+    lib.kivi_paged_append.argtypes = [VP] * 5
+    lib.kivi_paged_attention.argtypes = [VP] * 5 + [ctypes.c_size_t, VP]
     for name in EXPORTS[1:]:
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
@@ -212,7 +213,7 @@ def kivi_decode_workspace_bytes(layout: kivi_layout_t) -> int:
 def _stream_handle(stream) -> Optional[int]:
     if stream is None:
         import torch
-        stream = torch.cuda.current_stream()
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))     # (current_stream() takes 2.8 us)
     return ctypes.c_void_p(stream.cuda_stream)
 
 
@@ -407,14 +408,26 @@ def kivi_decode_attention_ragged(layout, cache: Cache, states, q_fp16, softmax_s
 
 
 # ---- operators around the cache ----
+# Single-token calls take as long as their binding, so these pack the structs' fields directly.
+
+_TENSOR = "Pqqq"
+_NO_TENSOR = (0, 0, 0, 0)
+_JOB = struct.Struct(_TENSOR * 2 + "Pfiii")
+_TWO_JOBS = struct.Struct((_TENSOR * 2 + "Pfiii") * 2)
+_ONE_TENSOR = struct.Struct(_TENSOR)
+_PROMPT = struct.Struct("iiiiiii4xPPiiiif4x")
+_ROWS = struct.Struct(_TENSOR * 4 + "iii4xPP")
+_QUERY = struct.Struct("PPiiif")
+
 
 def _type_of(x) -> int:
     import torch
-    if x.dtype == torch.float16:
+    dtype = x.dtype
+    if dtype is torch.float16:
         return KIVI_TYPE_FP16
-    if x.dtype == torch.bfloat16:
+    if dtype is torch.bfloat16:
         return KIVI_TYPE_BF16
-    raise KiviError(KIVI_ERR_UNSUPPORTED, f"tensor of {x.dtype}")
+    raise KiviError(KIVI_ERR_UNSUPPORTED, f"tensor of {dtype}")
 
 
 def _on_device(*tensors):
@@ -422,15 +435,16 @@ def _on_device(*tensors):
     import torch
     here = torch.cuda.current_device()
     for x in tensors:
-        if x is not None and (not x.is_cuda or x.device.index != here):
+        if x is not None and x.get_device() != here:
             raise KiviError(KIVI_ERR_INVALID_ARG, f"tensor on {x.device}, the current device is cuda:{here}")
 
 
-def _rows(x, heads=None, rows=None):
-    """[rows, heads, 128] (any row and head strides) as a kivi_tensor_t."""
-    assert x.dim() == 3 and x.shape[2] == 128 and x.stride(2) == 1, "expected [rows, heads, 128] with contiguous channels"
-    assert (heads is None or x.shape[1] == heads) and (rows is None or x.shape[0] == rows), f"unexpected shape {tuple(x.shape)}"
-    return kivi_tensor_t(x.data_ptr(), 0, x.stride(1), x.stride(0))
+def _rows(x, rows, heads=0):
+    """[rows, heads, 128] (any row and head strides) as the fields of a kivi_tensor_t."""
+    n, h, d = x.shape
+    st, sh, sd = x.stride()
+    assert n == rows and (h == heads or not heads) and d == 128 and sd == 1, f"expected [{rows}, {heads or 'heads'}, 128] with contiguous channels"
+    return x.data_ptr(), 0, sh, st
 
 
 def _int32(x, n=None):
@@ -438,7 +452,7 @@ def _int32(x, n=None):
     if x is None:
         return None
     import torch
-    assert x.dtype == torch.int32 and x.is_contiguous() and (n is None or x.numel() >= n), "expected a contiguous int32 tensor"
+    assert x.dtype is torch.int32 and x.is_contiguous() and (n is None or x.numel() >= n), "expected a contiguous int32 tensor"
     return x.data_ptr()
 
 
@@ -451,9 +465,19 @@ class Rotation:
         assert table.dim() == 2 and table.dtype == torch.float32 and table.is_contiguous(), "expected a contiguous fp32 table"
         self.table = table
         self.interleaved = int(interleaved)
+        self._alone = self.c()
 
     def c(self, positions=None, rows=0) -> kivi_rotation_t:
+        if positions is None and hasattr(self, "_alone"):
+            return self._alone
         return kivi_rotation_t(self.table.data_ptr(), _int32(positions, rows), self.table.shape[0], self.table.shape[1], self.interleaved)
+
+
+def _weight(w, x):
+    if w is None:
+        return 0
+    assert w.dtype is x.dtype and w.numel() == 128 and w.is_contiguous(), "expected a weight [128] of the tensor's type"
+    return w.data_ptr()
 
 
 def kivi_norm_rotate(q, q_out, k=None, k_out=None, q_weight=None, k_weight=None, eps=1e-6, weight_offset=0.0,
@@ -461,16 +485,14 @@ def kivi_norm_rotate(q, q_out, k=None, k_out=None, q_weight=None, k_weight=None,
     """q, k: CUDA fp16 / bf16 [rows, heads, 128] (any row and head strides); q_out, k_out the same shapes, fp16 or bf16, maybe q
     and k themselves; weights: [128] in the type of q / k, or None (no norm); positions: int32 [rows]."""
     _on_device(q, q_out, k, k_out, q_weight, k_weight, positions, rotation.table if rotation else None)
-    rows = q.shape[0]
-    jobs = (kivi_norm_rotate_job_t * 2)()
-    n = 0
-    for x, y, w in ((q, q_out, q_weight), (k, k_out, k_weight)):
-        if x is None:
-            continue
-        assert w is None or (w.dtype == x.dtype and w.numel() == 128 and w.is_contiguous()), "expected a weight [128] of the tensor's type"
-        jobs[n] = kivi_norm_rotate_job_t(_rows(x, rows=rows), _rows(y, x.shape[1], rows), w.data_ptr() if w is not None else None,
-                                         weight_offset, x.shape[1], _type_of(x), _type_of(y))
-        n += 1
+    rows, heads, _ = q.shape
+    job = (*_rows(q, rows), *_rows(q_out, rows, heads), _weight(q_weight, q), weight_offset, heads, _type_of(q), _type_of(q_out))
+    if k is None:
+        n, jobs = 1, _JOB.pack(*job)
+    else:
+        heads = k.shape[1]
+        n, jobs = 2, _TWO_JOBS.pack(*job, *_rows(k, rows), *_rows(k_out, rows, heads), _weight(k_weight, k), weight_offset, heads,
+                                    _type_of(k), _type_of(k_out))
     r = None
     if rotation is not None:
         assert positions is not None, "a rotation needs positions"
@@ -483,32 +505,33 @@ def kivi_prompt_attention(q, k, v, out, softmax_scale, q_starts=None, k_starts=N
     [b + 1]), rows of sequences one after the other: q, out [rows, H_q, 128], k, v [rows, H_kv, 128] and max_q, max_k the longest
     sequence's.  fp16 or bf16, all alike."""
     _on_device(q, k, v, out, q_starts, k_starts)
-    p = kivi_prompt_t(head_dim=128, type=_type_of(q), window=window, sinks=sinks, softmax_scale=softmax_scale)
-    assert _type_of(k) == _type_of(v) == _type_of(out) == p.type, "q, k, v and out have one type"
-    assert out.shape == q.shape and v.shape == k.shape, "out is shaped like q, v like k"
+    kind = _type_of(q)
+    assert _type_of(k) == _type_of(v) == _type_of(out) == kind, "q, k, v and out have one type"
     if q_starts is not None:
-        assert k_starts is not None and q_starts.numel() == k_starts.numel() and max_q is not None and max_k is not None
-        p.batch, p.n_q_heads, p.n_kv_heads = q_starts.numel() - 1, q.shape[1], k.shape[1]
-        p.max_q, p.max_k, p.q_rows, p.k_rows = max_q, max_k, q.shape[0], k.shape[0]
-        p.q_starts, p.k_starts = _int32(q_starts), _int32(k_starts)
-        tensors = [_rows(x) for x in (q, k, v, out)]
+        assert k_starts is not None and max_q is not None and max_k is not None, "both starts, and the longest sequence's lengths"
+        batch = q_starts.numel() - 1
+        q_rows, heads, _ = q.shape
+        k_rows, kv_heads, _ = k.shape
+        p = _PROMPT.pack(batch, heads, kv_heads, 128, kind, max_q, max_k, _int32(q_starts), _int32(k_starts, batch + 1), q_rows, k_rows, window, sinks,
+                         softmax_scale)
+        tensors = _rows(q, q_rows), _rows(k, k_rows), _rows(v, k_rows, kv_heads), _rows(out, q_rows, heads)
     else:
-        assert k_starts is None and q.dim() == 4 and q.shape[0] == k.shape[0] and q.shape[3] == k.shape[3] == 128
-        p.batch, p.n_q_heads, p.max_q = q.shape[:3]
-        p.n_kv_heads, p.max_k = k.shape[1:3]
-        tensors = [kivi_tensor_t(x.data_ptr(), *_strides_bht(x)) for x in (q, k, v, out)]
+        assert k_starts is None and out.shape == q.shape and v.shape == k.shape, "out is shaped like q, v like k"
+        batch, heads, max_q, d = q.shape
+        assert k.shape[0] == batch and k.shape[3] == d == 128, "expected [b, h, t, 128]"
+        p = _PROMPT.pack(batch, heads, k.shape[1], 128, kind, max_q, k.shape[2], 0, 0, 0, 0, window, sinks, softmax_scale)
+        tensors = [(x.data_ptr(), *_strides_bht(x)) for x in (q, k, v, out)]
     lib = load_library()
     need = ctypes.c_size_t(0)
-    _check(lib.kivi_prompt_workspace_bytes(ctypes.byref(p), ctypes.byref(need)), "kivi_prompt_workspace_bytes")
+    _check(lib.kivi_prompt_workspace_bytes(p, ctypes.byref(need)), "kivi_prompt_workspace_bytes")
     workspace = None
     if need.value:
         import torch
         workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-    handle = _stream_handle(stream)
-    if workspace is not None and stream is not None:
-        workspace.record_stream(stream)
-    _check(lib.kivi_prompt_attention(ctypes.byref(p), *(ctypes.byref(t) for t in tensors),
-                                     workspace.data_ptr() if workspace is not None else None, need.value, handle), "kivi_prompt_attention")
+        if stream is not None:
+            workspace.record_stream(stream)
+    _check(lib.kivi_prompt_attention(p, *[_ONE_TENSOR.pack(*t) for t in tensors], workspace.data_ptr() if need.value else None, need.value,
+                                     _stream_handle(stream)), "kivi_prompt_attention")
     return out
 
 
@@ -539,7 +562,11 @@ class PagedCache:
             assert given.is_cuda and given.is_contiguous() and given.numel() * given.element_size() >= n, f"{name}: {n} contiguous bytes"
             self.buffers[name] = given
             setattr(self.c, name, given.data_ptr())
-        self.workspace = torch.zeros(sizes.workspace, dtype=torch.uint8, device=self.buffers["pages"].device)
+        devices = {x.device for x in self.buffers.values()}
+        assert len(devices) == 1, "one device"
+        self.workspace = torch.zeros(sizes.workspace, dtype=torch.uint8, device=devices.pop())
+        self._refs = ctypes.byref(self.layout), ctypes.byref(self.c)
+        self._workspace = self.workspace.data_ptr(), self.workspace.numel()
 
     def records(self):
         """The pages as int32 words [n_pages, H_kv, records per page, words of a record]."""
@@ -557,15 +584,19 @@ class PagedCache:
 
 
 class PagedBatch:
-    """The sequences of a call: page_table int32 [b, max_pages] (rows may be strided), lengths int32 [b], slots int32 [b] or None."""
+    """The sequences of a call: page_table int32 [b, max_pages] (rows may be strided), lengths int32 [b], slots int32 [b] or None.  The
+    tensors are kept, not copied: what they hold when a call runs is what counts."""
 
     def __init__(self, page_table, lengths, slots=None):
         import torch
         n = lengths.numel()
         assert page_table.dim() == 2 and page_table.shape[0] == n and page_table.dtype == torch.int32 and (page_table.shape[1] < 2 or page_table.stride(1) == 1)
+        assert page_table.device == lengths.device and (slots is None or slots.device == lengths.device), "one device"
         self.page_table, self.lengths, self.slots = page_table, lengths, slots
+        self.size = n
         self.c = kivi_paged_batch_t(n, page_table.shape[1], max(page_table.stride(0), page_table.shape[1]), page_table.data_ptr(),
                                     _int32(lengths), _int32(slots, n))
+        self._ref = ctypes.byref(self.c)
 
 
 def kivi_paged_append(cache: PagedCache, batch: PagedBatch, k, v, starts=None, max_new=1, rotation: Optional[Rotation] = None, positions=None,
@@ -575,26 +606,28 @@ def kivi_paged_append(cache: PagedCache, batch: PagedBatch, k, v, starts=None, m
     already.  q [rows, H_q, 128] is rotated into q_out (fp16)."""
     _on_device(k, v, starts, positions, q, q_out, batch.lengths, cache.workspace, rotation.table if rotation else None)
     l, n = cache.layout, k.shape[0]
-    assert v.dtype == k.dtype and (q is None or q.dtype == k.dtype), "k, v and q have one type"
-    assert (q is None) == (q_out is None) and (q_out is None or _type_of(q_out) == KIVI_TYPE_FP16), "q goes into an fp16 q_out"
-    rows = kivi_paged_rows_t(k=_rows(k, l.n_kv_heads), v=_rows(v, l.n_kv_heads, n), type=_type_of(k), n_rows=n, max_new=max_new,
-                             starts=_int32(starts, batch.c.batch + 1))
+    heads = l.n_kv_heads
+    assert v.dtype is k.dtype, "k, v and q have one type"
+    qs = _NO_TENSOR * 2
     if q is not None:
-        rows.q, rows.q_out = _rows(q, l.n_q_heads, n), _rows(q_out, l.n_q_heads, n)
+        assert q.dtype is k.dtype and _type_of(q_out) == KIVI_TYPE_FP16, "q has the type of k, q_out is fp16"
+        qs = (*_rows(q, n, l.n_q_heads), *_rows(q_out, n, l.n_q_heads))
+    else:
+        assert q_out is None, "q_out without q"
+    r, at = None, 0
     if rotation is not None:
         r = rotation.c(positions, n)
-        rows.rotation = ctypes.pointer(r)
-    _check(load_library().kivi_paged_append(ctypes.byref(l), ctypes.byref(cache.c), ctypes.byref(batch.c), ctypes.byref(rows),
-                                            _stream_handle(stream)), "kivi_paged_append")
+        at = ctypes.addressof(r)
+    rows = _ROWS.pack(*_rows(k, n, heads), *_rows(v, n, heads), *qs, _type_of(k), n, max_new, _int32(starts, batch.size + 1) or 0, at)
+    _check(load_library().kivi_paged_append(*cache._refs, batch._ref, rows, _stream_handle(stream)), "kivi_paged_append")
 
 
 def kivi_paged_attention(cache: PagedCache, batch: PagedBatch, q_fp16, softmax_scale, out, window=0, sinks=0, stream=None):
     """q_fp16: contiguous CUDA fp16 [b, H_q, 128]; out: the same shape, contiguous, fp16 or bf16."""
     _on_device(q_fp16, out, batch.lengths, cache.workspace)
-    l = cache.layout
-    assert _type_of(q_fp16) == KIVI_TYPE_FP16 and q_fp16.is_contiguous() and out.is_contiguous()
-    assert tuple(q_fp16.shape) == tuple(out.shape) == (batch.c.batch, l.n_q_heads, 128), "q and out are [b, H_q, 128]"
-    query = kivi_paged_query_t(q_fp16.data_ptr(), out.data_ptr(), _type_of(out), window, sinks, softmax_scale)
-    _check(load_library().kivi_paged_attention(ctypes.byref(l), ctypes.byref(cache.c), ctypes.byref(batch.c), ctypes.byref(query),
-                                               cache.workspace.data_ptr(), cache.workspace.numel(), _stream_handle(stream)), "kivi_paged_attention")
+    assert _type_of(q_fp16) == KIVI_TYPE_FP16 and q_fp16.is_contiguous() and out.is_contiguous(), "q is fp16; q and out are contiguous"
+    shape = q_fp16.shape
+    assert shape == out.shape and shape == (batch.size, cache.layout.n_q_heads, 128), "q and out are [b, H_q, 128]"
+    query = _QUERY.pack(q_fp16.data_ptr(), out.data_ptr(), _type_of(out), window, sinks, softmax_scale)
+    _check(load_library().kivi_paged_attention(*cache._refs, batch._ref, query, *cache._workspace, _stream_handle(stream)), "kivi_paged_attention")
     return out
