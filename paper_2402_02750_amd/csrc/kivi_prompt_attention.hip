@@ -31,7 +31,26 @@ constexpr float kNothing = -1e30f;             // running maximum of a row that 
 
 struct Args : PromptParams {
     int32_t q_tiles;                   // of the longest sequence
+    int32_t by_die;                    // > 0: (sequence, kv-head) pairs per die, each pair's workgroups on one of the eight
 };
+
+// Asynchronous copy of 16 bytes per lane to LDS offset lds + 16 lane.  (Wait states between a vector instruction that writes the scalar operand and
+// this one: the compiler does not look into the block.  m0 is a reserved register, so the compiler warns that it keeps no value there: nor shall it.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void copy_to_lds(const void* base, uint32_t lane_offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(lane_offset), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void copy_to_lds(const void* lane_ptr, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(lane_ptr) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+// Workgroup barrier that orders LDS traffic only (a __syncthreads() would also wait for the copies in flight)
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
 
 template <bool BF16>
 __device__ __forceinline__ float16v product(uint4v a, uint4v b, float16v c) {
@@ -56,13 +75,22 @@ typedef __attribute__((address_space(3))) short4v* LdsShort4;
 
 template <bool BF16>
 __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attention_kernel(Args p) {
-    __shared__ __align__(16) unsigned char sm_k[kTileBytes], sm_v[kTileBytes];
+    __shared__ __align__(16) unsigned char sm[2][2][kTileBytes];          // [buffer][keys, values]
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    int at = blockIdx.x;
-    const int head = at % p.n_q_heads;
-    at /= p.n_q_heads;
-    const int b = at % p.batch, q_tile = p.q_tiles - 1 - at / p.batch;       // the longest rows first
+    const int rep = p.n_q_heads / p.n_kv_heads;
+    int at = blockIdx.x, b, head, q_tile;                                    // the longest rows first
+    if (p.by_die > 0) {
+        const int die = at & 7, in_die = at >> 3, r = in_die % rep, pair = in_die / rep % p.by_die * 8 + die;
+        b = pair / p.n_kv_heads;
+        head = (pair - b * p.n_kv_heads) * rep + r;
+        q_tile = p.q_tiles - 1 - in_die / rep / p.by_die;
+    } else {
+        head = at % p.n_q_heads;
+        at /= p.n_q_heads;
+        b = at % p.batch;
+        q_tile = p.q_tiles - 1 - at / p.batch;
+    }
     // the sequence
     int n_q = p.max_q, n_k = p.max_k;
     int64_t q_row = 0, k_row = 0;
@@ -79,7 +107,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attention_kernel(Args p
     }
     const int q0 = q_tile * kQueries;
     if (q0 >= n_q) return;
-    const int kv_head = head / (p.n_q_heads / p.n_kv_heads);
+    const int kv_head = head / rep;
     const int shift = n_k - n_q;                                   // query i stands at key i + shift
     const int first_at = q0 + shift, last_at = min(q0 + kQueries, n_q) - 1 + shift;
     const int my_q = q0 + wave * kWaveQueries + col, my_at = my_q + shift;
@@ -110,16 +138,38 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attention_kernel(Args p
     const __half* k_base = p.k.data + (p.k_starts ? 0 : b * p.k.stride_b) + kv_head * p.k.stride_h + k_row * p.k.stride_t;
     const __half* v_base = p.v.data + (p.k_starts ? 0 : b * p.v.stride_b) + kv_head * p.v.stride_h + k_row * p.v.stride_t;
 
-    for (int it = 0; it < n_tiles; ++it) {
-        const int key0 = (it < sink_tiles ? it : it - sink_tiles + first_tile) * kKeys;
-        __syncthreads();
+    // ---- copies: a wavefront has 16 rows of keys and of values, four per instruction ----
+    const uint32_t sm_lds = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)&sm[0][0][0]);
+    const int copy_row = lane >> 4, copy_slot = lane & 15;
+    uint32_t k_lane[4], v_lane;                                    // byte offsets of this lane's piece from the instruction's first row
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = wave * 16 + i * 4 + (lane >> 4), piece = lane & 15, key = min(key0 + row, n_k - 1);
-            *reinterpret_cast<uint4v*>(sm_k + key_offset(row, piece)) = *reinterpret_cast<const uint4v*>(k_base + key * p.k.stride_t + piece * 8);
-            *reinterpret_cast<uint4v*>(sm_v + value_offset(row, piece)) = *reinterpret_cast<const uint4v*>(v_base + key * p.v.stride_t + piece * 8);
+    for (int i = 0; i < 4; ++i) k_lane[i] = copy_row * (uint32_t)p.k.stride_t * 2 + ((copy_slot ^ (i * 4 + copy_row)) << 4);
+    v_lane = copy_row * (uint32_t)p.v.stride_t * 2 + ((copy_slot ^ (copy_row << 2)) << 4);
+    auto tile_key = [&](int it) { return (it < sink_tiles ? it : it - sink_tiles + first_tile) * kKeys; };
+    auto copy_tile = [&](int it, int buffer) {
+        const int row0 = tile_key(it) + wave * 16;
+        const uint32_t lds = sm_lds + buffer * 2 * kTileBytes + wave * 16 * 256;
+        if (row0 + 16 <= n_k) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) copy_to_lds(k_base + (row0 + i * 4) * p.k.stride_t, k_lane[i], lds + i * 1024);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) copy_to_lds(v_base + (row0 + i * 4) * p.v.stride_t, v_lane, lds + kTileBytes + i * 1024);
+        } else {                                                   // rows past the end re-read the last one
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int key = min(row0 + i * 4 + copy_row, n_k - 1);
+                copy_to_lds(k_base + key * p.k.stride_t + (copy_slot ^ (i * 4 + copy_row)) * 8, lds + i * 1024);
+                copy_to_lds(v_base + key * p.v.stride_t + (copy_slot ^ (copy_row << 2)) * 8, lds + kTileBytes + i * 1024);
+            }
         }
-        __syncthreads();
+    };
+    if (n_tiles > 0) copy_tile(0, 0);
+    for (int it = 0; it < n_tiles; ++it) {
+        const int key0 = tile_key(it);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // this wavefront's rows of the tile are there,
+        lds_barrier();                                             // everybody's, and nobody reads the other buffer any more
+        if (it + 1 < n_tiles) copy_tile(it + 1, (it + 1) & 1);
+        const unsigned char *sm_k = sm[it & 1][0], *sm_v = sm[it & 1][1];
         float16v s[2];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
@@ -202,6 +252,10 @@ hipError_t launch_prompt_attention(const PromptParams& params, void* workspace, 
     Args p{};
     static_cast<PromptParams&>(p) = params;
     p.q_tiles = (p.max_q + kQueries - 1) / kQueries;
+    // (the copies' lane offsets are 32 bits over four rows)
+    if (p.k.stride_t >= 1 << 28 || p.v.stride_t >= 1 << 28) return hipErrorNotSupported;
+    const int64_t pairs = (int64_t)p.batch * p.n_kv_heads;
+    p.by_die = pairs % 8 == 0 ? (int32_t)(pairs / 8) : 0;
     const int64_t blocks = (int64_t)p.batch * p.n_q_heads * p.q_tiles;
     if (blocks > 0x7fffffff) return hipErrorInvalidValue;
     if (p.bf16) prompt_attention_kernel<true><<<(unsigned)blocks, 64 * kWaves, 0, stream>>>(p);
