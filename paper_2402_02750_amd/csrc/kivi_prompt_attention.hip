@@ -141,53 +141,71 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attention_kernel(Args p
     // ---- copies: a wavefront has 16 rows of keys and of values, four per instruction ----
     const uint32_t sm_lds = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)&sm[0][0][0]);
     const int copy_row = lane >> 4, copy_slot = lane & 15;
-    uint32_t k_lane[4], v_lane;                                    // byte offsets of this lane's piece from the instruction's first row
+    uint32_t k_lane[4], v_lane[4];                                    // byte offsets of this lane's piece from the instruction's first row
 #pragma unroll
-    for (int i = 0; i < 4; ++i) k_lane[i] = copy_row * (uint32_t)p.k.stride_t * 2 + ((copy_slot ^ (i * 4 + copy_row)) << 4);
-    v_lane = copy_row * (uint32_t)p.v.stride_t * 2 + ((copy_slot ^ (copy_row << 2)) << 4);
+    for (int i = 0; i < 4; ++i) {
+        k_lane[i] = copy_row * (uint32_t)p.k.stride_t * 2 + ((copy_slot ^ (i * 4 + copy_row)) << 4);
+        v_lane[i] = copy_row * (uint32_t)p.v.stride_t * 2 + ((copy_slot ^ (copy_row << 2)) << 4);
+    }
     auto tile_key = [&](int it) { return (it < sink_tiles ? it : it - sink_tiles + first_tile) * kKeys; };
-    auto copy_tile = [&](int it, int buffer) {
+    auto copy_rows = [&](const __half* base, int64_t stride, const uint32_t (&lane_offset)[4], int it, uint32_t lds) {
         const int row0 = tile_key(it) + wave * 16;
-        const uint32_t lds = sm_lds + buffer * 2 * kTileBytes + wave * 16 * 256;
         if (row0 + 16 <= n_k) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) copy_to_lds(k_base + (row0 + i * 4) * p.k.stride_t, k_lane[i], lds + i * 1024);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) copy_to_lds(v_base + (row0 + i * 4) * p.v.stride_t, v_lane, lds + kTileBytes + i * 1024);
+            for (int i = 0; i < 4; ++i) copy_to_lds(base + (row0 + i * 4) * stride, lane_offset[i], lds + i * 1024);
         } else {                                                   // rows past the end re-read the last one
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int key = min(row0 + i * 4 + copy_row, n_k - 1);
-                copy_to_lds(k_base + key * p.k.stride_t + (copy_slot ^ (i * 4 + copy_row)) * 8, lds + i * 1024);
-                copy_to_lds(v_base + key * p.v.stride_t + (copy_slot ^ (copy_row << 2)) * 8, lds + kTileBytes + i * 1024);
+                copy_to_lds(base + key * stride + (int)(lane_offset[i] - copy_row * (uint32_t)stride * 2) / 2, lds + i * 1024);
             }
         }
     };
-    if (n_tiles > 0) copy_tile(0, 0);
-    for (int it = 0; it < n_tiles; ++it) {
-        const int key0 = tile_key(it);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // this wavefront's rows of the tile are there,
-        lds_barrier();                                             // everybody's, and nobody reads the other buffer any more
-        if (it + 1 < n_tiles) copy_tile(it + 1, (it + 1) & 1);
-        const unsigned char *sm_k = sm[it & 1][0], *sm_v = sm[it & 1][1];
-        float16v s[2];
+    auto copy_keys = [&](int it, int buffer) { copy_rows(k_base, p.k.stride_t, k_lane, it, sm_lds + buffer * 2 * kTileBytes + wave * 16 * 256); };
+    auto copy_values = [&](int it, int buffer) { copy_rows(v_base, p.v.stride_t, v_lane, it, sm_lds + (buffer * 2 + 1) * kTileBytes + wave * 16 * 256); };
+    float16v s[2];
+    // logits of a tile out of its keys in LDS
+    auto logits = [&](const unsigned char* sm_k, float16v (&to)[2]) {
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
+            for (int e = 0; e < 16; ++e) to[kb][e] = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                s[kb] = product<BF16>(*reinterpret_cast<const uint4v*>(sm_k + key_offset(kb * 32 + col, 2 * i + half)), qf[i], s[kb]);
+                to[kb] = product<BF16>(*reinterpret_cast<const uint4v*>(sm_k + key_offset(kb * 32 + col, 2 * i + half)), qf[i], to[kb]);
         }
-        // a tile that the mask cuts for some query of the workgroup
-        if (key0 + kKeys - 1 > first_at || (p.window > 0 && key0 <= last_at - p.window)) {
+    };
+    if (n_tiles > 0) {
+        copy_keys(0, 0);
+        copy_values(0, 0);
+        if (n_tiles > 1) copy_keys(1, 1);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        lds_barrier();
+        logits(sm[0][0], s);
+    }
+    for (int it = 0; it < n_tiles; ++it) {
+        const int key0 = tile_key(it);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // this wavefront's rows of the tiles are there,
+        lds_barrier();                                             // everybody's, and nobody reads the other buffers any more
+        if (it + 2 < n_tiles) copy_keys(it + 2, it & 1);
+        if (it + 1 < n_tiles) copy_values(it + 1, (it + 1) & 1);
+        const unsigned char *sm_v = sm[it & 1][1];
+        // tiles that the mask cuts for some query of the workgroup
+        if (key0 + kKeys - 1 > first_at) {
+            const int behind = my_at - key0 - 4 * half;            // the last visible key of the lane's, counted from its first
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[kb][e] = kb * 32 + (e & 3) + 8 * (e >> 2) <= behind ? s[kb][e] : -INFINITY;
+        }
+        if (p.window > 0 && key0 <= last_at - p.window) {
+            const int lowest_key = my_at - p.window + 1 - key0 - 4 * half, end_sinks = p.sinks - key0 - 4 * half;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int key = key0 + kb * 32 + (e & 3) + 8 * (e >> 2) + 4 * half;
-                    const bool sees = key <= my_at && (p.window == 0 || my_at - key < p.window || key < p.sinks);
-                    if (!sees) s[kb][e] = -INFINITY;
+                    const int key = kb * 32 + (e & 3) + 8 * (e >> 2);
+                    s[kb][e] = (key >= lowest_key) | (key < end_sinks) ? s[kb][e] : -INFINITY;
                 }
         }
         float mx = -INFINITY;
@@ -203,19 +221,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attention_kernel(Args p
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[i] *= f;
         }
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                s[kb][e] = __builtin_amdgcn_exp2f(fmaf(s[kb][e], c, -m));
-                l += s[kb][e];
-            }
+        uint4v pf[4];
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
             float pr[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) pr[e] = s[kk >> 1][(kk & 1) * 8 + e];
-            const uint4v pf = from_floats(pr, BF16);
+            for (int e = 0; e < 8; ++e) pr[e] = __builtin_amdgcn_exp2f(fmaf(s[kk >> 1][(kk & 1) * 8 + e], c, -m));
+            pf[kk] = from_floats(pr, BF16);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) l += pr[e];
+        }
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
             for (int cb = 0; cb < 4; ++cb) {
                 const int g = lane >> 4, i = lane & 15, channel = cb * 32 + 16 * (g & 1) + 4 * (i & 3);
@@ -225,9 +242,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attention_kernel(Args p
                     const int row = kk * 16 + 8 * r + 4 * (g >> 1) + (i >> 2);
                     vf.s4[r] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4)(sm_v + value_offset(row, channel >> 3) + (channel & 7) * 2));
                 }
-                o[cb] = product<BF16>(vf.v, pf, o[cb]);
+                o[cb] = product<BF16>(vf.v, pf[kk], o[cb]);
             }
-        }
+        if (it + 1 < n_tiles) logits(sm[(it + 1) & 1][0], s);
     }
     l = add_halves(l);
     if (my_q < n_q) {
