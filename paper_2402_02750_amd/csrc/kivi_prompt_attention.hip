@@ -1,10 +1,11 @@
 // Attention of prompts over 16-bit keys and values (kivi_prompt_attention): one pass over the keys with the running maximum and sum
 // of a softmax, causal, with an optional window and first keys that stay visible.
 //
-// A workgroup has 128 queries of one head, 32 per wavefront, and walks over tiles of 64 keys that all four wavefronts read
-// from LDS.  All products are 32x32x16 matrix instructions, and everything is kept transposed so that a query is a lane:
-//   S^T = K Q^T    operand rows are keys (out of LDS), columns are queries (in registers): lane (q = lane % 32, h = lane / 32) gets
-//                  the logits of keys 8 (i / 4) + 4 h + i % 4, i = 0..15: half of its query's; the other half is 32 lanes away
+// A row is a query of one head; rows of the heads that share a kv-head stand side by side (row = query * heads + head), so that a tile of rows
+// spans few queries: less of a tile is cut off by the mask, and keys and values are read once for all of them.  A wavefront has 32 rows.
+// All products are 32x32x16 matrix instructions, and everything is kept transposed so that a row is a lane:
+//   S^T = K Q^T    operand rows are keys (out of LDS), columns are rows (in registers): lane (col = lane % 32, half = lane / 32) gets
+//                  the logits of keys 8 (i / 4) + 4 half + i % 4, i = 0..15: half of its row's; the other half is 32 lanes away
 //   O^T = V^T P^T  the probabilities of a lane are, in the order the lane has them, its share of the second operand of an instruction over
 //                  16 keys, so they change neither lane nor order; the value rows are taken in that order too, transposed by the LDS read
 //                  (4 keys of one channel per lane and read).
@@ -12,9 +13,13 @@
 // starts at a finite number, so that rows which have seen nothing yet stay 0.  It moves only where a logit passes it by more
 // than 2^8 (the probabilities are at most 2^8 then, which both types hold); sums and outputs are fp32.
 // Probabilities are rounded to the tensors' type, to nearest: an error of 2^-12 (bf16: 2^-9) of each term at most.
+//
+// Two kernels.  prompt_tiles_kernel: a workgroup has 128 rows and walks over tiles of 64 keys that its four wavefronts share.
+// prompt_rows_kernel, where those workgroups would not fill the device: 32 rows, the wavefronts take the tiles (of 32 keys) in turn, each with buffers
+// of its own and without barriers, and join in LDS; with a workspace, several workgroups share the keys of the same rows, and a second launch joins them.
 #include "kivi_prompt.h"
 
-#include <type_traits>
+#include <algorithm>
 
 namespace kivi {
 namespace {
@@ -23,15 +28,19 @@ using namespace head_rows;
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef short short4v __attribute__((ext_vector_type(4)));
 
-constexpr int kWaves = 4, kWaveQueries = 32, kQueries = kWaves * kWaveQueries, kKeys = 64;
-constexpr int kTileBytes = kKeys * kHeadDim * 2;
+constexpr int kWaves = 4, kWaveRows = 32, kRowBytes = kHeadDim * 2;
+constexpr int kComputeUnits = 256;
+constexpr int kSplitTiles = 2;                 // tiles per wavefront, at least, before the keys of a tile of rows are split
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.f;                  // log2 headroom of the running maximum
 constexpr float kNothing = -1e30f;             // running maximum of a row that has seen nothing
 
 struct Args : PromptParams {
-    int32_t q_tiles;                   // of the longest sequence
-    int32_t by_die;                    // > 0: (sequence, kv-head) pairs per die, each pair's workgroups on one of the eight
+    FastDiv by_rep;
+    int32_t pairs, row_tiles;          // (sequence, kv-head) pairs; tiles of rows of the longest sequence
+    int32_t by_die;                    // > 0: pairs per die, each pair's workgroups on one of the eight
+    int32_t splits;
+    float *part_o, *part_ml;           // workspace: [pair][tile][row][split] outputs; maximum and sum
 };
 
 // Asynchronous copy of 16 bytes per lane to LDS offset lds + 16 lane.  (Wait states between a vector instruction that writes the scalar operand and
@@ -73,144 +82,143 @@ __device__ __forceinline__ int value_offset(int row, int piece) { return row * 2
 
 typedef __attribute__((address_space(3))) short4v* LdsShort4;
 
-template <bool BF16>
-__global__ __launch_bounds__(64 * kWaves, 2) void prompt_attention_kernel(Args p) {
-    __shared__ __align__(16) unsigned char sm[2][2][kTileBytes];          // [buffer][keys, values]
-    const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+// What a workgroup of 32 or 128 rows has to do
+struct Work {
+    int b, kv_head, n_q, n_k;
+    int64_t q_row, k_row;              // first rows of the sequence in the tensors
+    int row0, rows;                    // first row, rows of the sequence and kv-head
+    int shift, first_at, last_at;      // query i stands at key i + shift; the first and last of the workgroup's
+    bool valid;
+};
+__device__ __forceinline__ Work work_of(const Args& p, int pair, int tile, int tile_rows) {
+    Work w;
     const int rep = p.n_q_heads / p.n_kv_heads;
-    int at = blockIdx.x, b, head, q_tile;                                    // the longest rows first
-    if (p.by_die > 0) {
-        const int die = at & 7, in_die = at >> 3, r = in_die % rep, pair = in_die / rep % p.by_die * 8 + die;
-        b = pair / p.n_kv_heads;
-        head = (pair - b * p.n_kv_heads) * rep + r;
-        q_tile = p.q_tiles - 1 - in_die / rep / p.by_die;
-    } else {
-        head = at % p.n_q_heads;
-        at /= p.n_q_heads;
-        b = at % p.batch;
-        q_tile = p.q_tiles - 1 - at / p.batch;
-    }
-    // the sequence
-    int n_q = p.max_q, n_k = p.max_k;
-    int64_t q_row = 0, k_row = 0;
+    w.b = pair / p.n_kv_heads;
+    w.kv_head = pair - w.b * p.n_kv_heads;
+    w.n_q = p.max_q;
+    w.n_k = p.max_k;
+    w.q_row = w.k_row = 0;
+    w.valid = true;
     if (p.q_starts) {
-        const int first = p.q_starts[b], end = p.q_starts[b + 1];
-        n_q = first >= 0 && end <= p.q_rows && end >= first && (int64_t)end - first <= p.max_q ? end - first : 0;
-        q_row = first;
+        const int first = p.q_starts[w.b], end = p.q_starts[w.b + 1];
+        w.valid = first >= 0 && end <= p.q_rows && end >= first && (int64_t)end - first <= p.max_q;
+        w.n_q = end - first;
+        w.q_row = first;
     }
     if (p.k_starts) {
-        const int first = p.k_starts[b], end = p.k_starts[b + 1];
-        if (!(first >= 0 && end <= p.k_rows && end >= first && (int64_t)end - first <= p.max_k)) return;
-        n_k = end - first;
-        k_row = first;
+        const int first = p.k_starts[w.b], end = p.k_starts[w.b + 1];
+        w.valid = w.valid && first >= 0 && end <= p.k_rows && end >= first && (int64_t)end - first <= p.max_k;
+        w.n_k = end - first;
+        w.k_row = first;
     }
-    const int q0 = q_tile * kQueries;
-    if (q0 >= n_q) return;
-    const int kv_head = head / rep;
-    const int shift = n_k - n_q;                                   // query i stands at key i + shift
-    const int first_at = q0 + shift, last_at = min(q0 + kQueries, n_q) - 1 + shift;
-    const int my_q = q0 + wave * kWaveQueries + col, my_at = my_q + shift;
-
-    // queries: columns of the first product
-    const float c = fmaxf(fabsf(p.softmax_scale) * kLog2e, 1e-30f);        // (not 0: masked logits stay -inf)
-    uint4v qf[8];
-    {
-        const __half* src = p.q.data + (p.q_starts ? 0 : b * p.q.stride_b) + head * p.q.stride_h + (q_row + min(my_q, n_q - 1)) * p.q.stride_t + half * 8;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            qf[i] = *reinterpret_cast<const uint4v*>(src + i * 16);
-            if (p.softmax_scale < 0.f) qf[i] ^= 0x80008000u;
-        }
+    w.rows = w.valid ? w.n_q * rep : 0;
+    w.row0 = tile * tile_rows;
+    w.valid = w.valid && w.row0 < w.rows;
+    w.shift = w.n_k - w.n_q;
+    w.first_at = p.by_rep.of(w.row0) + w.shift;
+    w.last_at = p.by_rep.of(min(w.row0 + tile_rows, max(w.rows, 1)) - 1) + w.shift;
+    return w;
+}
+// The tiles of KEYS keys that some row of the workgroup sees: those of the first keys, then those that the window reaches
+template <int KEYS>
+struct Tiles {
+    int sinks, first, count;           // tiles of the first keys; the first one of the window; all
+    __device__ __forceinline__ Tiles(const Args& p, const Work& w) {
+        const int lowest = p.window > 0 ? max(w.first_at - p.window + 1, 0) : 0, end = w.last_at < 0 ? 0 : w.last_at / KEYS + 1;
+        sinks = p.window > 0 ? min((min(p.sinks, lowest) + KEYS - 1) / KEYS, end) : 0;
+        first = max(lowest / KEYS, sinks);
+        count = sinks + max(end - first, 0);
     }
-    float16v o[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
-    float m = kNothing, l = 0.f;
+    __device__ __forceinline__ int key(int i) const { return (i < sinks ? i : i - sinks + first) * KEYS; }
+};
+__device__ __forceinline__ const __half* base_of(const TensorParams& t, const int32_t* starts, const Work& w) {
+    return t.data + (starts ? 0 : w.b * t.stride_b) + w.kv_head * t.stride_h + w.k_row * t.stride_t;
+}
 
-    // key tiles: those of the first keys, then those that the window reaches
-    const int lowest = p.window > 0 ? max(first_at - p.window + 1, 0) : 0;
-    const int sink_tiles = p.window > 0 ? (min(p.sinks, lowest) + kKeys - 1) / kKeys : 0;
-    const int first_tile = max(lowest / kKeys, sink_tiles), end_tile = last_at < 0 ? 0 : last_at / kKeys + 1;
-    const int n_tiles = last_at < 0 ? 0 : min(sink_tiles, end_tile) + max(end_tile - first_tile, 0);
-    const __half* k_base = p.k.data + (p.k_starts ? 0 : b * p.k.stride_b) + kv_head * p.k.stride_h + k_row * p.k.stride_t;
-    const __half* v_base = p.v.data + (p.k_starts ? 0 : b * p.v.stride_b) + kv_head * p.v.stride_h + k_row * p.v.stride_t;
-
-    // ---- copies: a wavefront has 16 rows of keys and of values, four per instruction ----
-    const uint32_t sm_lds = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)&sm[0][0][0]);
-    const int copy_row = lane >> 4, copy_slot = lane & 15;
-    uint32_t k_lane[4], v_lane[4];                                    // byte offsets of this lane's piece from the instruction's first row
+// Copies of 16 rows of a tensor (four per instruction) into LDS.  swap(row): by how much the pieces of a row change place
+template <class Swap>
+struct Copier {
+    uint32_t lane_offset[4];
+    __device__ __forceinline__ Copier(int64_t stride, int lane, Swap swap) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        k_lane[i] = copy_row * (uint32_t)p.k.stride_t * 2 + ((copy_slot ^ (i * 4 + copy_row)) << 4);
-        v_lane[i] = copy_row * (uint32_t)p.v.stride_t * 2 + ((copy_slot ^ (copy_row << 2)) << 4);
+        for (int i = 0; i < 4; ++i) lane_offset[i] = (lane >> 4) * (uint32_t)stride * 2 + (((lane & 15) ^ swap(i * 4 + (lane >> 4))) << 4);
     }
-    auto tile_key = [&](int it) { return (it < sink_tiles ? it : it - sink_tiles + first_tile) * kKeys; };
-    auto copy_rows = [&](const __half* base, int64_t stride, const uint32_t (&lane_offset)[4], int it, uint32_t lds) {
-        const int row0 = tile_key(it) + wave * 16;
-        if (row0 + 16 <= n_k) {
+    __device__ __forceinline__ void copy(const __half* base, int64_t stride, int row0, int n_rows, int lane, uint32_t lds) const {
+        if (row0 + 16 <= n_rows) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) copy_to_lds(base + (row0 + i * 4) * stride, lane_offset[i], lds + i * 1024);
         } else {                                                   // rows past the end re-read the last one
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int key = min(row0 + i * 4 + copy_row, n_k - 1);
-                copy_to_lds(base + key * stride + (int)(lane_offset[i] - copy_row * (uint32_t)stride * 2) / 2, lds + i * 1024);
+                const int row = min(row0 + i * 4 + (lane >> 4), n_rows - 1);
+                copy_to_lds(base + row * stride + (int)(lane_offset[i] - (lane >> 4) * (uint32_t)stride * 2) / 2, lds + i * 1024);
             }
         }
-    };
-    auto copy_keys = [&](int it, int buffer) { copy_rows(k_base, p.k.stride_t, k_lane, it, sm_lds + buffer * 2 * kTileBytes + wave * 16 * 256); };
-    auto copy_values = [&](int it, int buffer) { copy_rows(v_base, p.v.stride_t, v_lane, it, sm_lds + (buffer * 2 + 1) * kTileBytes + wave * 16 * 256); };
-    float16v s[2];
-    // logits of a tile out of its keys in LDS
-    auto logits = [&](const unsigned char* sm_k, float16v (&to)[2]) {
+    }
+};
+struct KeySwap { __device__ __forceinline__ int operator()(int row) const { return row & 15; } };
+struct ValueSwap { __device__ __forceinline__ int operator()(int row) const { return (row & 3) << 2; } };
+
+// 32 rows of a wavefront; KB: halves of 32 keys in a tile
+template <bool BF16, int KB>
+struct Rows {
+    uint4v qf[8];                      // columns of the first product
+    float16v o[4];                     // o[cb][i]: channel 32 cb + 8 (i / 4) + 4 half + i % 4
+    float c, m, l;
+    int at;                            // where this lane's query stands
+
+    __device__ __forceinline__ void start(const Args& p, const Work& w, int row, int half) {
+        const int query = p.by_rep.of(min(row, w.rows - 1)), r = min(row, w.rows - 1) - query * (p.n_q_heads / p.n_kv_heads);
+        at = query + w.shift;
+        const __half* src = p.q.data + (p.q_starts ? 0 : w.b * p.q.stride_b) + (w.kv_head * (p.n_q_heads / p.n_kv_heads) + r) * p.q.stride_h +
+                            (w.q_row + query) * p.q.stride_t + half * 8;
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
+        for (int i = 0; i < 8; ++i) {
+            qf[i] = *reinterpret_cast<const uint4v*>(src + i * 16);
+            if (p.softmax_scale < 0.f) qf[i] ^= 0x80008000u;
+        }
 #pragma unroll
-            for (int e = 0; e < 16; ++e) to[kb][e] = 0.f;
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+        c = fmaxf(fabsf(p.softmax_scale) * kLog2e, 1e-30f);        // (not 0: masked logits stay -inf)
+        m = kNothing;
+        l = 0.f;
+    }
+    __device__ __forceinline__ void logits(const unsigned char* sm_k, int lane, float16v (&s)[KB]) const {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                to[kb] = product<BF16>(*reinterpret_cast<const uint4v*>(sm_k + key_offset(kb * 32 + col, 2 * i + half)), qf[i], to[kb]);
+                s[kb] = product<BF16>(*reinterpret_cast<const uint4v*>(sm_k + key_offset(kb * 32 + (lane & 31), 2 * i + (lane >> 5))), qf[i], s[kb]);
         }
-    };
-    if (n_tiles > 0) {
-        copy_keys(0, 0);
-        copy_values(0, 0);
-        if (n_tiles > 1) copy_keys(1, 1);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        lds_barrier();
-        logits(sm[0][0], s);
     }
-    for (int it = 0; it < n_tiles; ++it) {
-        const int key0 = tile_key(it);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // this wavefront's rows of the tiles are there,
-        lds_barrier();                                             // everybody's, and nobody reads the other buffers any more
-        if (it + 2 < n_tiles) copy_keys(it + 2, it & 1);
-        if (it + 1 < n_tiles) copy_values(it + 1, (it + 1) & 1);
-        const unsigned char *sm_v = sm[it & 1][1];
-        // tiles that the mask cuts for some query of the workgroup
-        if (key0 + kKeys - 1 > first_at) {
-            const int behind = my_at - key0 - 4 * half;            // the last visible key of the lane's, counted from its first
+    // what the mask hides of a tile that begins with key0
+    __device__ __forceinline__ void mask(const Args& p, const Work& w, int key0, int half, float16v (&s)[KB]) const {
+        if (key0 + KB * 32 - 1 > w.first_at) {
+            const int behind = at - key0 - 4 * half;               // the last visible key, counted from the lane's first
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+            for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[kb][e] = kb * 32 + (e & 3) + 8 * (e >> 2) <= behind ? s[kb][e] : -INFINITY;
         }
-        if (p.window > 0 && key0 <= last_at - p.window) {
-            const int lowest_key = my_at - p.window + 1 - key0 - 4 * half, end_sinks = p.sinks - key0 - 4 * half;
+        if (p.window > 0 && key0 <= w.last_at - p.window) {
+            const int lowest = at - p.window + 1 - key0 - 4 * half, end_sinks = p.sinks - key0 - 4 * half;
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+            for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int key = kb * 32 + (e & 3) + 8 * (e >> 2);
-                    s[kb][e] = (key >= lowest_key) | (key < end_sinks) ? s[kb][e] : -INFINITY;
+                    s[kb][e] = ((key >= lowest) | (key < end_sinks)) ? s[kb][e] : -INFINITY;
                 }
         }
+    }
+    __device__ __forceinline__ void raise(const float16v (&s)[KB]) {
         float mx = -INFINITY;
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
         mx = max_halves(mx) * c;
@@ -221,9 +229,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attention_kernel(Args p
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[i] *= f;
         }
-        uint4v pf[4];
+    }
+    __device__ __forceinline__ void add(const unsigned char* sm_v, int lane, const float16v (&s)[KB]) {
+        uint4v pf[2 * KB];
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
+        for (int kk = 0; kk < 2 * KB; ++kk) {
             float pr[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) pr[e] = __builtin_amdgcn_exp2f(fmaf(s[kk >> 1][(kk & 1) * 8 + e], c, -m));
@@ -232,7 +242,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attention_kernel(Args p
             for (int e = 0; e < 8; ++e) l += pr[e];
         }
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk)
+        for (int kk = 0; kk < 2 * KB; ++kk)
 #pragma unroll
             for (int cb = 0; cb < 4; ++cb) {
                 const int g = lane >> 4, i = lane & 15, channel = cb * 32 + 16 * (g & 1) + 4 * (i & 3);
@@ -244,39 +254,255 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attention_kernel(Args p
                 }
                 o[cb] = product<BF16>(vf.v, pf[kk], o[cb]);
             }
-        if (it + 1 < n_tiles) logits(sm[(it + 1) & 1][0], s);
     }
-    l = add_halves(l);
-    if (my_q < n_q) {
+};
+// four channels of a row
+template <bool BF16>
+__device__ __forceinline__ void store_four(__half* dst, float a, float b, float c, float d) {
+    const float r[8] = {a, b, c, d, 0.f, 0.f, 0.f, 0.f};
+    const uint4v w = from_floats(r, BF16);
+    *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ __half* out_row(const Args& p, const Work& w, int row) {
+    const int rep = p.n_q_heads / p.n_kv_heads, query = p.by_rep.of(row), r = row - query * rep;
+    return p.out.data + (p.q_starts ? 0 : w.b * p.out.stride_b) + (w.kv_head * rep + r) * p.out.stride_h + (w.q_row + query) * p.out.stride_t;
+}
+__device__ __forceinline__ uint32_t lds_address(unsigned char* p) {
+    return (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)p);
+}
+// (pair, tile) of a workgroup: the tiles with the most keys first; by_die: all workgroups of a pair on one die, whose L2 then has its keys
+__device__ __forceinline__ void place_of(const Args& p, int at, int& pair, int& tile) {
+    if (p.by_die > 0) {
+        pair = (at >> 3) % p.by_die * 8 + (at & 7);
+        tile = p.row_tiles - 1 - (at >> 3) / p.by_die;
+    } else {
+        pair = at % p.pairs;
+        tile = p.row_tiles - 1 - at / p.pairs;
+    }
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(64 * kWaves, 2) void prompt_tiles_kernel(Args p) {
+    constexpr int kKeys = 64, kTileBytes = kKeys * kRowBytes;
+    __shared__ __align__(16) unsigned char sm[2][2][kTileBytes];          // [buffer][keys, values]
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int pair, tile;
+    place_of(p, blockIdx.x, pair, tile);
+    const Work w = work_of(p, pair, tile, kWaves * kWaveRows);
+    if (!w.valid) return;
+    const int row = w.row0 + wave * kWaveRows + (lane & 31);
+    Rows<BF16, 2> r;
+    r.start(p, w, row, half);
+    const Tiles<kKeys> tiles(p, w);
+    const __half *k_base = base_of(p.k, p.k_starts, w), *v_base = base_of(p.v, p.k_starts, w);
+    const Copier<KeySwap> keys(p.k.stride_t, lane, KeySwap{});
+    const Copier<ValueSwap> values(p.v.stride_t, lane, ValueSwap{});
+    const uint32_t lds = lds_address(&sm[0][0][0]) + wave * 16 * kRowBytes;
+    auto copy_keys = [&](int i) { keys.copy(k_base, p.k.stride_t, tiles.key(i) + wave * 16, w.n_k, lane, lds + (i & 1) * 2 * kTileBytes); };
+    auto copy_values = [&](int i) { values.copy(v_base, p.v.stride_t, tiles.key(i) + wave * 16, w.n_k, lane, lds + ((i & 1) * 2 + 1) * kTileBytes); };
+    float16v s[2], next[2];
+    if (tiles.count > 0) {
+        copy_keys(0);
+        copy_values(0);
+        if (tiles.count > 1) copy_keys(1);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        lds_barrier();
+        r.logits(sm[0][0], lane, s);
+    }
+    for (int i = 0; i < tiles.count; ++i) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // this wavefront's rows of the tiles are there,
+        lds_barrier();                                             // everybody's, and nobody reads the other buffers any more
+        if (i + 2 < tiles.count) copy_keys(i + 2);
+        if (i + 1 < tiles.count) copy_values(i + 1);
+        r.mask(p, w, tiles.key(i), half, s);
+        r.raise(s);
+        r.logits(sm[(i + 1) & 1][0], lane, next);                  // (after the last tile: of what the buffer holds, not used)
+        r.add(sm[i & 1][1], lane, s);
+        s[0] = next[0];
+        s[1] = next[1];
+    }
+    const float l = add_halves(r.l);
+    if (row < w.rows) {
         const float f = l > 0.f ? 1.f / l : 0.f;
-        __half* dst = p.out.data + (p.q_starts ? 0 : b * p.out.stride_b) + head * p.out.stride_h + (q_row + my_q) * p.out.stride_t;
+        __half* dst = out_row(p, w, row) + 4 * half;
 #pragma unroll
         for (int cb = 0; cb < 4; ++cb)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float r[8] = {o[cb][4 * i] * f, o[cb][4 * i + 1] * f, o[cb][4 * i + 2] * f, o[cb][4 * i + 3] * f, 0.f, 0.f, 0.f, 0.f};
-                const uint4v w = from_floats(r, BF16);
-                *reinterpret_cast<uint2*>(dst + cb * 32 + 8 * i + 4 * half) = make_uint2(w[0], w[1]);
-            }
+            for (int i = 0; i < 4; ++i) store_four<BF16>(dst + cb * 32 + 8 * i, r.o[cb][4 * i] * f, r.o[cb][4 * i + 1] * f, r.o[cb][4 * i + 2] * f, r.o[cb][4 * i + 3] * f);
     }
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(64 * kWaves, 1) void prompt_rows_kernel(Args p) {
+    constexpr int kKeys = 32, kTileBytes = kKeys * kRowBytes;
+    __shared__ __align__(16) unsigned char sm[kWaves][2][2][kTileBytes];  // [wavefront][buffer][keys, values]; then outputs [wavefront][channel][row]
+    __shared__ float sm_ml[kWaves][2][kWaveRows];
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int pair, tile;
+    const int at = (int)blockIdx.x / p.splits, split = (int)blockIdx.x - at * p.splits;
+    place_of(p, at, pair, tile);
+    const Work w = work_of(p, pair, tile, kWaveRows);
+    if (!w.valid) return;
+    Rows<BF16, 1> r;
+    r.start(p, w, w.row0 + col, half);
+    const Tiles<kKeys> tiles(p, w);
+    // this workgroup's tiles: [from, to), of them every fourth
+    const int from = (int)((int64_t)tiles.count * split / p.splits), to = (int)((int64_t)tiles.count * (split + 1) / p.splits);
+    const __half *k_base = base_of(p.k, p.k_starts, w), *v_base = base_of(p.v, p.k_starts, w);
+    const Copier<KeySwap> keys(p.k.stride_t, lane, KeySwap{});
+    const Copier<ValueSwap> values(p.v.stride_t, lane, ValueSwap{});
+    const uint32_t lds = lds_address(&sm[wave][0][0][0]);
+    auto copy_tile = [&](int i, int buffer) {                      // 16 instructions
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            keys.copy(k_base, p.k.stride_t, tiles.key(i) + x * 16, w.n_k, lane, lds + buffer * 2 * kTileBytes + x * 16 * kRowBytes);
+            values.copy(v_base, p.v.stride_t, tiles.key(i) + x * 16, w.n_k, lane, lds + (buffer * 2 + 1) * kTileBytes + x * 16 * kRowBytes);
+        }
+    };
+    int buffer = 0;
+    if (from + wave < to) copy_tile(from + wave, 0);
+    for (int i = from + wave; i < to; i += kWaves) {
+        if (i + kWaves < to) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the other buffer's last reads are done
+            copy_tile(i + kWaves, buffer ^ 1);
+            asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        float16v s[1];
+        r.logits(sm[wave][buffer][0], lane, s);
+        r.mask(p, w, tiles.key(i), half, s);
+        r.raise(s);
+        r.add(sm[wave][buffer][1], lane, s);
+        buffer ^= 1;
+    }
+    // ---- join the wavefronts ----
+    const float lw = add_halves(r.l);
+    float* mine = reinterpret_cast<float*>(&sm[wave][0][0][0]);    // [channel][row]
+    static_assert(kHeadDim * kWaveRows * sizeof(float) <= sizeof(sm[0]), "outputs of a wavefront");
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int cb = 0; cb < 4; ++cb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mine[(cb * 32 + 8 * (e >> 2) + 4 * half + (e & 3)) * kWaveRows + col] = r.o[cb][e];
+    if (half == 0) {
+        sm_ml[wave][0][col] = r.m;
+        sm_ml[wave][1][col] = lw;
+    }
+    __syncthreads();
+    // wavefront cb has channels 32 cb + 16 half .. of all rows
+    float m = kNothing, l = 0.f, f[kWaves], o[16];
+#pragma unroll
+    for (int x = 0; x < kWaves; ++x) m = fmaxf(m, sm_ml[x][0][col]);
+#pragma unroll
+    for (int x = 0; x < kWaves; ++x) {
+        f[x] = __builtin_amdgcn_exp2f(sm_ml[x][0][col] - m);
+        l = fmaf(sm_ml[x][1][col], f[x], l);
+    }
+    const int c0 = wave * 32 + half * 16;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        o[e] = 0.f;
+#pragma unroll
+        for (int x = 0; x < kWaves; ++x) o[e] = fmaf(reinterpret_cast<const float*>(&sm[x][0][0][0])[(c0 + e) * kWaveRows + col], f[x], o[e]);
+    }
+    const int row = w.row0 + col;
+    if (row >= w.rows) return;
+    if (p.splits == 1) {
+        const float g = l > 0.f ? 1.f / l : 0.f;
+        __half* dst = out_row(p, w, row) + c0;
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) store_four<BF16>(dst + e, o[e] * g, o[e + 1] * g, o[e + 2] * g, o[e + 3] * g);
+    } else {
+        const int64_t part = (((int64_t)pair * p.row_tiles + tile) * kWaveRows + col) * p.splits + split;
+        float4v* dst = reinterpret_cast<float4v*>(p.part_o + part * kHeadDim + c0);
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) dst[e / 4] = float4v{o[e], o[e + 1], o[e + 2], o[e + 3]};
+        if (c0 == 0) *reinterpret_cast<float2*>(p.part_ml + part * 2) = make_float2(m, l);
+    }
+}
+
+// Joins the parts of prompt_rows_kernel: 32 lanes per row, four channels each
+template <bool BF16>
+__global__ __launch_bounds__(256) void prompt_join_kernel(Args p) {
+    const int at = (int)blockIdx.x * 8 + (int)(threadIdx.x >> 5), c = (threadIdx.x & 31) * 4;
+    const int tile_at = at / kWaveRows, pair = tile_at / p.row_tiles, tile = tile_at - pair * p.row_tiles;
+    if (pair >= p.pairs) return;
+    const Work w = work_of(p, pair, tile, kWaveRows);
+    const int row = w.row0 + at % kWaveRows;
+    if (!w.valid || row >= w.rows) return;
+    const int64_t part = (((int64_t)pair * p.row_tiles + tile) * kWaveRows + at % kWaveRows) * p.splits;
+    float m = kNothing, l = 0.f;
+    for (int s = 0; s < p.splits; ++s) m = fmaxf(m, p.part_ml[(part + s) * 2]);
+    float4v o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = 0; s < p.splits; ++s) {
+        const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + (part + s) * 2);
+        const float f = __builtin_amdgcn_exp2f(ml.x - m);
+        l = fmaf(ml.y, f, l);
+        o += *reinterpret_cast<const float4v*>(p.part_o + (part + s) * kHeadDim + c) * f;
+    }
+    const float f = l > 0.f ? 1.f / l : 0.f;
+    store_four<BF16>(out_row(p, w, row) + c, o[0] * f, o[1] * f, o[2] * f, o[3] * f);
+}
+
+// What a call runs: tiles of 128 rows, or of 32 with `splits` workgroups each
+struct Plan { bool small; int splits; };
+Plan plan_of(const PromptParams& p) {
+    const int64_t rows = (int64_t)p.max_q * (p.n_q_heads / p.n_kv_heads), pairs = (int64_t)p.batch * p.n_kv_heads;
+    Plan plan{false, 1};
+    plan.small = pairs * ((rows + 127) / 128) < kComputeUnits;
+    if (plan.small) {
+        // keys that a tile of rows sees at most, in tiles
+        int64_t keys = p.max_k;
+        if (p.window > 0) keys = std::min<int64_t>(keys, (int64_t)p.window + kWaveRows + std::min(p.sinks, p.max_k));
+        const int64_t tiles = (keys + 31) / 32, groups = pairs * ((rows + 31) / 32);
+        plan.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kComputeUnits / groups, tiles / (kWaves * kSplitTiles)));
+    }
+    return plan;
 }
 
 }  // namespace
 
-size_t prompt_workspace_bytes(const PromptParams& p) { return 0; }
+size_t prompt_workspace_bytes(const PromptParams& p) {
+    const Plan plan = plan_of(p);
+    if (plan.splits == 1) return 0;
+    const size_t rows = (size_t)p.max_q * (p.n_q_heads / p.n_kv_heads), tiles = (rows + kWaveRows - 1) / kWaveRows;
+    return (size_t)p.batch * p.n_kv_heads * tiles * kWaveRows * plan.splits * (kHeadDim + 2) * sizeof(float);
+}
 
 hipError_t launch_prompt_attention(const PromptParams& params, void* workspace, size_t workspace_bytes, hipStream_t stream) {
     Args p{};
     static_cast<PromptParams&>(p) = params;
-    p.q_tiles = (p.max_q + kQueries - 1) / kQueries;
-    // (the copies' lane offsets are 32 bits over four rows)
-    if (p.k.stride_t >= 1 << 28 || p.v.stride_t >= 1 << 28) return hipErrorNotSupported;
-    const int64_t pairs = (int64_t)p.batch * p.n_kv_heads;
+    // (the copies' lane offsets are 32 bits over four rows; rows are counted in 31 bits)
+    const int rep = p.n_q_heads / p.n_kv_heads;
+    const int64_t rows = (int64_t)p.max_q * rep, pairs = (int64_t)p.batch * p.n_kv_heads;
+    if (p.k.stride_t >= 1 << 28 || p.v.stride_t >= 1 << 28 || rows > 0x3fffffff || pairs > 0x7fffffff) return hipErrorNotSupported;
+    Plan plan = plan_of(p);
+    if (!workspace || workspace_bytes < prompt_workspace_bytes(p)) plan.splits = 1;
+    const int tile_rows = plan.small ? kWaveRows : kWaves * kWaveRows;
+    p.by_rep = FastDiv::by(rep);
+    p.pairs = (int32_t)pairs;
+    p.row_tiles = (int32_t)((rows + tile_rows - 1) / tile_rows);
+    p.splits = plan.splits;
     p.by_die = pairs % 8 == 0 ? (int32_t)(pairs / 8) : 0;
-    const int64_t blocks = (int64_t)p.batch * p.n_q_heads * p.q_tiles;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    if (p.bf16) prompt_attention_kernel<true><<<(unsigned)blocks, 64 * kWaves, 0, stream>>>(p);
-    else prompt_attention_kernel<false><<<(unsigned)blocks, 64 * kWaves, 0, stream>>>(p);
+    const int64_t blocks = pairs * p.row_tiles * plan.splits;
+    if (blocks > 0x7fffffff) return hipErrorNotSupported;
+    if (!plan.small) {
+        if (p.bf16) prompt_tiles_kernel<true><<<(unsigned)blocks, 64 * kWaves, 0, stream>>>(p);
+        else prompt_tiles_kernel<false><<<(unsigned)blocks, 64 * kWaves, 0, stream>>>(p);
+        return hipGetLastError();
+    }
+    p.part_o = static_cast<float*>(workspace);
+    p.part_ml = p.part_o + (size_t)pairs * p.row_tiles * kWaveRows * plan.splits * kHeadDim;
+    if (p.bf16) prompt_rows_kernel<true><<<(unsigned)blocks, 64 * kWaves, 0, stream>>>(p);
+    else prompt_rows_kernel<false><<<(unsigned)blocks, 64 * kWaves, 0, stream>>>(p);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess || plan.splits == 1) return e;
+    const int64_t join_blocks = pairs * p.row_tiles * kWaveRows / 8;
+    if (p.bf16) prompt_join_kernel<true><<<(unsigned)join_blocks, 256, 0, stream>>>(p);
+    else prompt_join_kernel<false><<<(unsigned)join_blocks, 256, 0, stream>>>(p);
     return hipGetLastError();
 }
 
