@@ -30,7 +30,9 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 4, kWaveRows = 32, kRowBytes = kHeadDim * 2;
 constexpr int kComputeUnits = 256;
-constexpr int kSplitTiles = 2;                 // tiles per wavefront, at least, before the keys of a tile of rows are split
+// Tiles per wavefront, at least, before the keys of a tile of rows are split.  (One query, 8000 keys before it, 32 / 8 heads, and five queries, 7000 keys,
+// 4 heads: not split 84 and 73 us; 2: 19.4, 17.5; 4: 18.5, 17.0; 8: 22.4, 22.3.)
+constexpr int kSplitTiles = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.f;                  // log2 headroom of the running maximum
 constexpr float kNothing = -1e30f;             // running maximum of a row that has seen nothing
@@ -453,7 +455,9 @@ struct Plan { bool small; int splits; };
 Plan plan_of(const PromptParams& p) {
     const int64_t rows = (int64_t)p.max_q * (p.n_q_heads / p.n_kv_heads), pairs = (int64_t)p.batch * p.n_kv_heads;
     Plan plan{false, 1};
-    plan.small = pairs * ((rows + 127) / 128) < kComputeUnits;
+    // (124 workgroups of 128 rows, 4 heads x 3900 tokens: 79.8 us, in rows of 32 50.6; 64 of them, 2000 tokens: 44.4, 25.9; 160, 2 x 600, 16 / 8 heads: 18.0,
+    // 21.9; 220, 7000 tokens, window 500: 24.0, 44.3)
+    plan.small = pairs * ((rows + 127) / 128) <= kComputeUnits / 2;
     if (plan.small) {
         // keys that a tile of rows sees at most, in tiles
         int64_t keys = p.max_k;
