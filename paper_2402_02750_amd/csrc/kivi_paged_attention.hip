@@ -35,8 +35,12 @@ union Frag {                           // one lane's share of an operand: eight 
 
 constexpr int kWaves = 4;
 constexpr int kWorkgroups = 768;       // three per compute unit; a multiple of the eight dies
-constexpr int kMinCost = 4;            // of an interval
-constexpr int kRowCost = 3;            // of a step of fp16 rows, in steps of records
+// Costs in steps of records.  Of a step of fp16 rows (1, 2, 3, 4: 16 x 32 767 tokens, 64 / 8 heads, 4 bits 125.7, 126.8, 130.3, 126.3 us; 32 x 16 001 tokens,
+// window 4096 108, 101, 105, 107; 200 x 500-2000 tokens 75, 72, 74), and what a further unit in an interval costs (leaving one, entering the next).
+constexpr int kRowCost = 2, kEnterCost = 5;
+// Steps of an interval, at least (1, 2, 4, 8: one sequence of 3001 tokens 15.3, 15.3, 18.2, 25 us; 4 heads x 1023 tokens 11.0, 9.9, 11.7, 17; 8000 tokens, 32 / 8 heads 21.9, 18.0, 20.7, 26)
+constexpr int kMinCost = 2;
+constexpr int kScanned = 4;            // times 64 sequences whose costs stay in registers
 constexpr int kMaxHeads = 8;           // query heads of a unit
 constexpr int kPartFloats = kHeadDim;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -69,6 +73,17 @@ __device__ __forceinline__ float max_rows(float x) {
     x = fmaxf(__int_as_float(a[0]), __int_as_float(a[1]));
     auto b = __builtin_amdgcn_permlane32_swap(__float_as_int(x), __float_as_int(x), false, false);
     return fmaxf(__int_as_float(b[0]), __int_as_float(b[1]));
+}
+// sum of this and the lanes before
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int add_from(int x) { return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false); }
+__device__ __forceinline__ int sum_upto(int x) {
+    x = add_from<0x111, 0xF>(x);       // 1, 2, 4, 8 lanes before, within 16
+    x = add_from<0x112, 0xF>(x);
+    x = add_from<0x114, 0xF>(x);
+    x = add_from<0x118, 0xF>(x);
+    x = add_from<0x142, 0xA>(x);       // the last of 16 to the next 16, the last of 32 to the next 32
+    return add_from<0x143, 0xC>(x);
 }
 __device__ __forceinline__ half2v pack_rtz(float a, float b) { return __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(a, b)); }
 __device__ __forceinline__ float2 load_shared(const float* p) {      // of what another workgroup has stored
@@ -193,34 +208,68 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
 
     // ---- this workgroup's interval of the axis ----
     const int wg = ((int)blockIdx.x & 7) * (kWorkgroups / 8) + ((int)blockIdx.x >> 3);      // neighbours on the axis share a die
-    auto cost_of = [&](int b) { return b < p.batch ? view_of(p, p.lengths[b], p.slots ? p.slots[b] : b).cost() * units_per_sequence : 0; };
-    auto sum_upto = [&](int x) {                                       // of this and the lanes before
+    auto cost_of = [&](int b) { return b < p.batch ? view_of(p, p.lengths[b], p.slots ? p.slots[b] : b).cost() : 0; };
+    auto sum_all = [&](int x) { return __builtin_amdgcn_readlane(sum_upto(x), 63); };
+    int costs[kScanned];                                               // of the first sequences, 64 at a time
+    int total = 0, units = 0;
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int y = __shfl_up(x, d);
-            if (lane >= d) x += y;
+    for (int i = 0; i < kScanned; ++i) {
+        costs[i] = 0;
+        if (i * 64 < p.batch) {
+            costs[i] = cost_of(i * 64 + lane);
+            total += sum_all(costs[i]) * units_per_sequence;
+            units += __popcll(__ballot(costs[i] > 0)) * units_per_sequence;
         }
-        return x;
-    };
-    const int cost0 = cost_of(lane), upto0 = sum_upto(cost0);
-    int total = __shfl(upto0, 63);
-    for (int b0 = 64; b0 < p.batch; b0 += 64) total += __shfl(sum_upto(cost_of(b0 + lane)), 63);
-    total = __builtin_amdgcn_readfirstlane(total);
-    const int length = max((total + kWorkgroups - 1) / kWorkgroups, kMinCost);
-    const int x0 = wg * length, x1 = min(x0 + length, total);
-    if (x0 >= x1) return;
-    int b = 0, before = 0;                                             // the sequence of x0, and where it begins
-    for (int b0 = 0, sum = 0; b0 < p.batch; b0 += 64) {
-        const int mine = b0 ? cost_of(b0 + lane) : cost0, upto = b0 ? sum_upto(mine) : upto0;
-        const uint64_t here = __ballot(sum + upto > x0);
-        if (here) {
-            const int at = __builtin_ctzll(here);
-            b = b0 + at;
-            before = sum + __shfl(upto - mine, at);
-            break;
-        }
-        sum += __shfl(upto, 63);
     }
+    for (int b0 = kScanned * 64; b0 < p.batch; b0 += 64) total += sum_all(cost_of(b0 + lane)) * units_per_sequence;
+    if (total == 0) return;
+    // An interval of `length` of the axis for every workgroup, or, where that costs little more, every unit cut evenly on its own: `length`
+    // is then the longest piece, and no workgroup enters two units.
+    int length = max((total + kWorkgroups - 1) / kWorkgroups, kMinCost);
+    bool own_pieces = false;
+    if (p.batch <= kScanned * 64 && units < kWorkgroups) {
+        auto fits = [&](int piece) {
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < kScanned; ++i)
+                if (i * 64 < p.batch) n += sum_all((costs[i] + piece - 1) / piece) * units_per_sequence;
+            return n <= kWorkgroups;
+        };
+        own_pieces = fits(length + kEnterCost);
+        if (own_pieces) {
+            int low = length, high = length + kEnterCost;
+            while (low < high) {
+                const int mid = (low + high) / 2;
+                if (fits(mid)) high = mid;
+                else low = mid + 1;
+            }
+            length = low;
+        }
+    }
+    // what of the axis is in front of a sequence: workgroups with pieces of their own, cost otherwise
+    auto share_of = [&](int cost) { return (own_pieces ? (cost + length - 1) / length : cost) * units_per_sequence; };
+    const int x_first = own_pieces ? wg : wg * length;
+    int b = -1, before = 0;                                            // the sequence of this workgroup's first unit, and where it begins
+    {
+        int sum = 0;
+        auto look = [&](int b0, int cost) {
+            const int mine = share_of(cost), upto = sum_upto(mine);
+            const uint64_t here = __ballot(sum + upto > x_first);
+            if (here) {
+                const int at = __builtin_ctzll(here);
+                b = b0 + at;
+                before = sum + __builtin_amdgcn_readlane(upto - mine, at);
+            }
+            sum += __builtin_amdgcn_readlane(upto, 63);
+        };
+#pragma unroll
+        for (int i = 0; i < kScanned; ++i)
+            if (b < 0 && i * 64 < p.batch) look(i * 64, costs[i]);
+        for (int b0 = kScanned * 64; b < 0 && b0 < p.batch; b0 += 64) look(b0, cost_of(b0 + lane));
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+    before = __builtin_amdgcn_readfirstlane(before);
+    if (b < 0) return;                                                 // (more workgroups than pieces, or than intervals)
     // A place on the axis: sequence, unit in it, and where the unit begins
     struct Place { int b, unit, unit0; View view; };
     auto next_unit = [&](Place& u) {                                   // (only where another one follows)
@@ -233,15 +282,29 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
             } while (u.view.cost() == 0);
         }
     };
+    Place here;
+    here.b = b;
+    here.view = view_of(p, scalar(p.lengths, here.b), p.slots ? scalar(p.slots, here.b) : here.b);
+    int x0, x1, pieces = 1, piece = 0;                                 // the interval; own pieces: of the unit
+    {
+        const int cost = here.view.cost();
+        if (own_pieces) {
+            pieces = (cost + length - 1) / length;
+            here.unit = (wg - before) / pieces;
+            piece = wg - before - here.unit * pieces;
+            here.unit0 = 0;
+            x0 = cost * piece / pieces;
+            x1 = cost * (piece + 1) / pieces;
+        } else {
+            here.unit = (x_first - before) / cost;
+            here.unit0 = before + here.unit * cost;
+            x0 = x_first;
+            x1 = min(x0 + length, total);
+        }
+    }
     // its steps of records in this interval: [first, end)
     auto records_from = [&](const Place& u) { return max(x0 - u.unit0 - u.view.row_steps * kRowCost, 0); };
     auto records_to = [&](const Place& u) { return max(min(x1 - u.unit0, u.view.cost()) - u.view.row_steps * kRowCost, 0); };
-    Place here;
-    here.b = __builtin_amdgcn_readfirstlane(b);
-    here.view = view_of(p, scalar(p.lengths, here.b), p.slots ? scalar(p.slots, here.b) : here.b);
-    before = __builtin_amdgcn_readfirstlane(before);
-    here.unit = (x0 - before) / here.view.cost();
-    here.unit0 = before + here.unit * here.view.cost();
 
     // ---- copies of records into this wavefront's ring, NB ahead ----
     const uint32_t ring_lds = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)&sm_ring[wave][0][0]);
@@ -655,7 +718,8 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
                 sm_ml[wave][lane][1] = lw;
             }
         }
-        const int owner0 = here.unit0 / length, parts = (here.unit0 + cost - 1) / length - owner0 + 1;
+        const int owner0 = own_pieces ? wg - piece : here.unit0 / length;         // the first workgroup of the unit
+        const int parts = own_pieces ? pieces : (here.unit0 + cost - 1) / length - owner0 + 1;
         auto write_out = [&](int hh, int c, float ox, float oy, float sum) {
             const float f = sum > 0.f ? 1.f / sum : 0.f;
             const int64_t i = (q_row + hh) * kHeadDim + c;
@@ -708,7 +772,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
             lds_barrier();
             if (sm_last) {
                 // the unit is the first one of every workgroup but, maybe, the first of them
-                const int second = owner0 * length < here.unit0 ? 1 : 0;
+                const int second = !own_pieces && owner0 * length < here.unit0 ? 1 : 0;
                 constexpr int kBatch = 8;
                 for (int hh = wave; hh < live; hh += kWaves) {
                     float mm = kNothing, sum = 0.f, ox = 0.f, oy = 0.f;
