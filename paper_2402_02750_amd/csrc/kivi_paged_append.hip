@@ -9,7 +9,8 @@
 //           values of tokens that stay in the window
 // The roles do not wait for each other.  Rows are stored at slot t % cap_r, groups read slots of tokens before the call: the first read
 // is at most n + R + 30 tokens before the last one written, so one launch is right while that is less than cap_r; otherwise
-// the rows are a launch after the groups.
+// the rows are a launch after the groups.  (One wavefront for the groups that read slots and the rows that replace them, all in one launch: its
+// registers slowed the groups down, 16 x 4096 tokens, 32 heads 305 us against 266.)
 //
 // The packed codes are a bit contract, so the rotation is one too: fp32 products and one difference, each rounded on its own
 // (this file is compiled without contraction), then one rounding to fp16.
@@ -25,9 +26,10 @@ using namespace head_rows;
 using tile::half2v;
 
 struct Args : PagedAppendParams {
-    int32_t group_blocks;              // workgroups of the first role
+    FastDiv by_kv_heads, by_groups, by_tokens, by_pieces;
     int32_t groups, tokens, pieces;    // per sequence: groups, tokens looked at; per token: runs of eight heads
-    int64_t group_waves, row_waves;
+    int32_t row_heads;                 // q, k and v
+    int32_t group_blocks, group_waves, row_waves;
 };
 
 struct Sequence {
@@ -90,15 +92,7 @@ __device__ __forceinline__ half2v turned_pair(const RotationParams& r, uint32_t 
 }
 
 template <int BITS>
-__device__ __forceinline__ void group_role(const Args& p, int64_t at, int lane) {
-    const int kv = (int)(at & 1);
-    at >>= 1;
-    const int h = (int)(at % p.n_kv_heads);
-    at /= p.n_kv_heads;
-    const int g = (int)(at % p.groups), b = (int)(at / p.groups);
-    const Sequence s = sequence_of(p, b);
-    const int record = packed_records(s.before, p.residual) + g;
-    if (!s.valid || record >= packed_records(s.after, p.residual)) return;
+__device__ __forceinline__ void pack_group(const Args& p, const Sequence& s, int b, int h, int kv, int record, int lane) {
     const int entry = record >> p.page_shift;
     if (entry >= p.max_pages) return;
     const int page = p.page_table[b * p.page_table_stride + entry];
@@ -160,27 +154,17 @@ __device__ __forceinline__ void group_role(const Args& p, int64_t at, int lane) 
     }
 }
 
-__device__ __forceinline__ void row_role(const Args& p, int64_t at, int lane) {
-    const int piece = (int)(at % p.pieces);
-    at /= p.pieces;
-    const int from_end = (int)(at % p.tokens), b = (int)(at / p.tokens);
-    const Sequence s = sequence_of(p, b);
-    const int t = s.after - 1 - from_end;              // its place in the sequence
-    if (!s.valid || t < s.before) return;
-    const bool stays = t >= packed_records(s.after, p.residual) * kTileTokens;
-    const int n_q = p.q_out.data ? p.n_q_heads : 0, head = piece * 8 + (lane >> 3), j = lane & 7;
-    const int64_t row = (int64_t)s.first_row + t - s.before;
-    const bool is_q = head < n_q, is_k = !is_q && head < n_q + p.n_kv_heads;
-    if (head >= n_q + 2 * p.n_kv_heads || (!is_q && !stays)) return;
-    const TensorParams& from = is_q ? p.q : is_k ? p.k : p.v;
-    const int h = is_q ? head : is_k ? head - n_q : head - n_q - p.n_kv_heads;
+// One row by eight lanes: of a query (which 0), key (1) or value (2) head h of new row `row`, token t of its sequence
+__device__ __forceinline__ void store_row(const Args& p, const Sequence& s, int which, int h, int64_t row, int t, int lane) {
+    const int j = lane & 7;
+    const TensorParams& from = which == 0 ? p.q : which == 1 ? p.k : p.v;
     const __half* src = from.data + row * from.stride_t + h * from.stride_h;
     __half* dst;
-    if (is_q) dst = p.q_out.data + row * p.q_out.stride_t + h * p.q_out.stride_h;
-    else dst = (is_k ? p.k_resid : p.v_resid) + (((int64_t)s.slot * p.n_kv_heads + h) * p.cap_r + t % p.cap_r) * kHeadDim;
+    if (which == 0) dst = p.q_out.data + row * p.q_out.stride_t + h * p.q_out.stride_h;
+    else dst = (which == 1 ? p.k_resid : p.v_resid) + (((int64_t)s.slot * p.n_kv_heads + h) * p.cap_r + t % p.cap_r) * kHeadDim;
     const Pieces pc = pieces_of(j, p.rotates ? p.rotation.half : 0, p.rotation.interleaved);
     uint4v a4 = *reinterpret_cast<const uint4v*>(src + pc.a * 8), b4 = *reinterpret_cast<const uint4v*>(src + pc.b * 8);
-    const bool turns = p.rotates && (is_q || is_k) && j < p.rotation.half / 8;
+    const bool turns = p.rotates && which != 2 && j < p.rotation.half / 8;
     if (turns || p.bf16) {
         float x[8], y[8];
         to_floats(a4, p.bf16, x);
@@ -198,13 +182,34 @@ __device__ __forceinline__ void row_role(const Args& p, int64_t at, int lane) {
 }
 
 template <int BITS>
+__device__ __forceinline__ void group_role(const Args& p, int at, int lane) {
+    const int kv = at & 1;
+    at >>= 1;
+    const int by_heads = p.by_kv_heads.of(at), h = at - by_heads * p.n_kv_heads, b = p.by_groups.of(by_heads), g = by_heads - b * p.groups;
+    const Sequence s = sequence_of(p, b);
+    const int record = packed_records(s.before, p.residual) + g;
+    if (s.valid && record < packed_records(s.after, p.residual)) pack_group<BITS>(p, s, b, h, kv, record, lane);
+}
+
+__device__ __forceinline__ void row_role(const Args& p, int at, int lane) {
+    const int by_pieces = p.by_pieces.of(at), piece = at - by_pieces * p.pieces, b = p.by_tokens.of(by_pieces), from_end = by_pieces - b * p.tokens;
+    const Sequence s = sequence_of(p, b);
+    const int t = s.after - 1 - from_end, head = piece * 8 + (lane >> 3);
+    if (!s.valid || t < s.before || head >= p.row_heads) return;
+    const bool stays = t >= packed_records(s.after, p.residual) * kTileTokens;
+    const int n_q = p.q_out.data ? p.n_q_heads : 0, which = head < n_q ? 0 : head < n_q + p.n_kv_heads ? 1 : 2;
+    if (which > 0 && !stays) return;
+    store_row(p, s, which, which == 0 ? head : which == 1 ? head - n_q : head - n_q - p.n_kv_heads, (int64_t)s.first_row + t - s.before, t, lane);
+}
+
+template <int BITS, bool GROUPS, bool ROWS>
 __global__ __launch_bounds__(256) void paged_append_kernel(Args p) {
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if ((int)blockIdx.x < p.group_blocks) {
-        const int64_t at = (int64_t)blockIdx.x * 4 + wave;
+    if (GROUPS && (!ROWS || (int)blockIdx.x < p.group_blocks)) {
+        const int at = (int)blockIdx.x * 4 + wave;
         if (at < p.group_waves) group_role<BITS>(p, at, lane);
-    } else {
-        const int64_t at = (int64_t)((int)blockIdx.x - p.group_blocks) * 4 + wave;
+    } else if (ROWS) {
+        const int at = ((int)blockIdx.x - (GROUPS ? p.group_blocks : 0)) * 4 + wave;
         if (at < p.row_waves) row_role(p, at, lane);
     }
 }
@@ -214,23 +219,31 @@ __global__ __launch_bounds__(256) void paged_append_kernel(Args p) {
 hipError_t launch_paged_append(const PagedAppendParams& params, hipStream_t stream) {
     Args p{};
     static_cast<PagedAppendParams&>(p) = params;
-    p.groups = (p.max_new + kTileTokens - 1) / kTileTokens;
-    const int window = p.residual + kTileTokens - 1;            // rows that stay, at most
-    p.tokens = p.q_out.data ? p.max_new : std::min(p.max_new, window);
-    p.pieces = ((p.q_out.data ? p.n_q_heads : 0) + 2 * p.n_kv_heads + 7) / 8;
-    p.group_waves = (int64_t)p.batch * p.groups * p.n_kv_heads * 2;
-    p.row_waves = (int64_t)p.batch * p.tokens * p.pieces;
-    const int64_t group_blocks = (p.group_waves + 3) / 4, row_blocks = (p.row_waves + 3) / 4;
-    if (group_blocks + row_blocks > 0x7fffffff) return hipErrorInvalidValue;
-    auto launch = [&](int64_t groups, int64_t rows) {
-        p.group_blocks = (int32_t)groups;
-        if (p.bits == 2) paged_append_kernel<2><<<(unsigned)(groups + rows), 256, 0, stream>>>(p);
-        else paged_append_kernel<4><<<(unsigned)(groups + rows), 256, 0, stream>>>(p);
+    const bool queries = p.q_out.data != nullptr;
+    p.groups = (p.max_new - 1) / kTileTokens + 1;
+    p.tokens = queries ? p.max_new : std::min(p.max_new, p.residual + kTileTokens - 1);      // (rows that stay, at most)
+    p.row_heads = (queries ? p.n_q_heads : 0) + 2 * p.n_kv_heads;
+    p.pieces = (p.row_heads + 7) / 8;
+    const int64_t groups = (int64_t)p.batch * p.groups * p.n_kv_heads * 2, rows = (int64_t)p.batch * p.tokens * p.pieces;
+    if (groups + rows > 0x7ffffff0) return hipErrorNotSupported;
+    p.group_waves = (int32_t)groups;
+    p.row_waves = (int32_t)rows;
+    p.group_blocks = (int32_t)((groups + 3) / 4);
+    p.by_kv_heads = FastDiv::by(p.n_kv_heads);
+    p.by_groups = FastDiv::by(p.groups);
+    p.by_tokens = FastDiv::by(p.tokens);
+    p.by_pieces = FastDiv::by(p.pieces);
+    const unsigned group_blocks = (unsigned)p.group_blocks, row_blocks = (unsigned)((rows + 3) / 4);
+    if ((int64_t)p.max_new + p.residual + 30 < p.cap_r) {
+        if (p.bits == 2) paged_append_kernel<2, true, true><<<group_blocks + row_blocks, 256, 0, stream>>>(p);
+        else paged_append_kernel<4, true, true><<<group_blocks + row_blocks, 256, 0, stream>>>(p);
         return hipGetLastError();
-    };
-    if ((int64_t)p.max_new + p.residual + 30 < p.cap_r) return launch(group_blocks, row_blocks);
-    if (hipError_t e = launch(group_blocks, 0); e != hipSuccess) return e;
-    return launch(0, row_blocks);
+    }
+    if (p.bits == 2) paged_append_kernel<2, true, false><<<group_blocks, 256, 0, stream>>>(p);
+    else paged_append_kernel<4, true, false><<<group_blocks, 256, 0, stream>>>(p);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    paged_append_kernel<2, false, true><<<row_blocks, 256, 0, stream>>>(p);        // (the bits are the groups')
+    return hipGetLastError();
 }
 
 }  // namespace kivi
