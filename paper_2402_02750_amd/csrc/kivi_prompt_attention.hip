@@ -20,6 +20,7 @@
 #include "kivi_prompt.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace kivi {
 namespace {
@@ -137,25 +138,37 @@ __device__ __forceinline__ const __half* base_of(const TensorParams& t, const in
     return t.data + (starts ? 0 : w.b * t.stride_b) + w.kv_head * t.stride_h + w.k_row * t.stride_t;
 }
 
-// Copies of 16 rows of a tensor (four per instruction) into LDS.  swap(row): by how much the pieces of a row change place
+// Copies of 16 rows of a tensor (four per instruction) into LDS.  swap(row): by how much the pieces of a row change place.  Rows are taken in
+// order, `step` rows further each time; only skip() moves elsewhere.  (Scalar instructions count: with the rows' addresses made anew for every
+// tile a wavefront spent 148 of them per tile, a fifth of its time.)
 template <class Swap>
 struct Copier {
     uint32_t lane_offset[4];
-    __device__ __forceinline__ Copier(int64_t stride, int lane, Swap swap) {
+    const char* next;                  // the next rows
+    int64_t stride, advance;           // bytes from row to row, from step to step
+    int row;
+    __device__ __forceinline__ Copier(const __half* base, int64_t stride_t, int first, int step, int lane, Swap swap)
+        : next(reinterpret_cast<const char*>(base) + first * stride_t * 2), stride(stride_t * 2), advance(step * stride_t * 2), row(first) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) lane_offset[i] = (lane >> 4) * (uint32_t)stride * 2 + (((lane & 15) ^ swap(i * 4 + (lane >> 4))) << 4);
+        for (int i = 0; i < 4; ++i) lane_offset[i] = (uint32_t)(i * 4 + (lane >> 4)) * (uint32_t)stride + (((lane & 15) ^ swap(i * 4 + (lane >> 4))) << 4);
     }
-    __device__ __forceinline__ void copy(const __half* base, int64_t stride, int row0, int n_rows, int lane, uint32_t lds) const {
-        if (row0 + 16 <= n_rows) {
+    __device__ __forceinline__ void skip(int rows) {
+        next += rows * stride;
+        row += rows;
+    }
+    __device__ __forceinline__ void copy(int n_rows, int step, int lane, uint32_t lds) {
+        if (row + 16 <= n_rows) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) copy_to_lds(base + (row0 + i * 4) * stride, lane_offset[i], lds + i * 1024);
+            for (int i = 0; i < 4; ++i) copy_to_lds(next, lane_offset[i], lds + i * 1024);
         } else {                                                   // rows past the end re-read the last one
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int row = min(row0 + i * 4 + (lane >> 4), n_rows - 1);
-                copy_to_lds(base + row * stride + (int)(lane_offset[i] - (lane >> 4) * (uint32_t)stride * 2) / 2, lds + i * 1024);
+                const int r = i * 4 + (lane >> 4), there = min(r, n_rows - 1 - row);
+                copy_to_lds(next + there * stride + (int)(lane_offset[i] - (uint32_t)r * (uint32_t)stride), lds + i * 1024);
             }
         }
+        next += advance;
+        row += step;
     }
 };
 struct KeySwap { __device__ __forceinline__ int operator()(int row) const { return row & 15; } };
@@ -297,32 +310,46 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_tiles_kernel(Args p) {
     Rows<BF16, 2> r;
     r.start(p, w, row, half);
     const Tiles<kKeys> tiles(p, w);
-    const __half *k_base = base_of(p.k, p.k_starts, w), *v_base = base_of(p.v, p.k_starts, w);
-    const Copier<KeySwap> keys(p.k.stride_t, lane, KeySwap{});
-    const Copier<ValueSwap> values(p.v.stride_t, lane, ValueSwap{});
+    const int key_first = tiles.key(0) + wave * 16;
+    Copier<KeySwap> keys(base_of(p.k, p.k_starts, w), p.k.stride_t, key_first, kKeys, lane, KeySwap{});
+    Copier<ValueSwap> values(base_of(p.v, p.k_starts, w), p.v.stride_t, key_first, kKeys, lane, ValueSwap{});
     const uint32_t lds = lds_address(&sm[0][0][0]) + wave * 16 * kRowBytes;
-    auto copy_keys = [&](int i) { keys.copy(k_base, p.k.stride_t, tiles.key(i) + wave * 16, w.n_k, lane, lds + (i & 1) * 2 * kTileBytes); };
-    auto copy_values = [&](int i) { values.copy(v_base, p.v.stride_t, tiles.key(i) + wave * 16, w.n_k, lane, lds + ((i & 1) * 2 + 1) * kTileBytes); };
+    const int jump = (tiles.first - tiles.sinks) * kKeys;          // rows between the tiles of the first keys and the window's
+    auto copy_keys = [&](int i, int buffer) {
+        if (i == tiles.sinks && jump > 0 && i > 0) keys.skip(jump);
+        keys.copy(w.n_k, kKeys, lane, lds + buffer * 2 * kTileBytes);
+    };
+    auto copy_values = [&](int i, int buffer) {
+        if (i == tiles.sinks && jump > 0 && i > 0) values.skip(jump);
+        values.copy(w.n_k, kKeys, lane, lds + (buffer * 2 + 1) * kTileBytes);
+    };
+    const int count = tiles.count;
     float16v s[2], next[2];
-    if (tiles.count > 0) {
-        copy_keys(0);
-        copy_values(0);
-        if (tiles.count > 1) copy_keys(1);
+    if (count > 0) {
+        copy_keys(0, 0);
+        copy_values(0, 0);
+        if (count > 1) copy_keys(1, 1);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         lds_barrier();
         r.logits(sm[0][0], lane, s);
     }
-    for (int i = 0; i < tiles.count; ++i) {
+    // tile i, whose logits are there, and the next one's logits
+    auto step = [&](int i, auto parity, const float16v (&now)[2], float16v (&then)[2]) {
+        constexpr int B = decltype(parity)::value;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // this wavefront's rows of the tiles are there,
         lds_barrier();                                             // everybody's, and nobody reads the other buffers any more
-        if (i + 2 < tiles.count) copy_keys(i + 2);
-        if (i + 1 < tiles.count) copy_values(i + 1);
-        r.mask(p, w, tiles.key(i), half, s);
-        r.raise(s);
-        r.logits(sm[(i + 1) & 1][0], lane, next);                  // (after the last tile: of what the buffer holds, not used)
-        r.add(sm[i & 1][1], lane, s);
-        s[0] = next[0];
-        s[1] = next[1];
+        if (i + 2 < count) copy_keys(i + 2, B);
+        if (i + 1 < count) copy_values(i + 1, B ^ 1);
+        float16v x[2] = {now[0], now[1]};
+        r.mask(p, w, tiles.key(i), half, x);
+        r.raise(x);
+        r.logits(sm[B ^ 1][0], lane, then);                        // (after the last tile: of what the buffer holds, not used)
+        r.add(sm[B][1], lane, x);
+    };
+    for (int i = 0; i < count; i += 2) {
+        step(i, std::integral_constant<int, 0>{}, s, next);
+        if (i + 1 == count) break;
+        step(i + 1, std::integral_constant<int, 1>{}, next, s);
     }
     const float l = add_halves(r.l);
     if (row < w.rows) {
@@ -352,15 +379,16 @@ __global__ __launch_bounds__(64 * kWaves, 1) void prompt_rows_kernel(Args p) {
     const Tiles<kKeys> tiles(p, w);
     // this workgroup's tiles: [from, to), of them every fourth
     const int from = (int)((int64_t)tiles.count * split / p.splits), to = (int)((int64_t)tiles.count * (split + 1) / p.splits);
-    const __half *k_base = base_of(p.k, p.k_starts, w), *v_base = base_of(p.v, p.k_starts, w);
-    const Copier<KeySwap> keys(p.k.stride_t, lane, KeySwap{});
-    const Copier<ValueSwap> values(p.v.stride_t, lane, ValueSwap{});
+    Copier<KeySwap> keys(base_of(p.k, p.k_starts, w), p.k.stride_t, 0, 16, lane, KeySwap{});
+    Copier<ValueSwap> values(base_of(p.v, p.k_starts, w), p.v.stride_t, 0, 16, lane, ValueSwap{});
     const uint32_t lds = lds_address(&sm[wave][0][0][0]);
     auto copy_tile = [&](int i, int buffer) {                      // 16 instructions
+        keys.skip(tiles.key(i) - keys.row);
+        values.skip(tiles.key(i) - values.row);
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            keys.copy(k_base, p.k.stride_t, tiles.key(i) + x * 16, w.n_k, lane, lds + buffer * 2 * kTileBytes + x * 16 * kRowBytes);
-            values.copy(v_base, p.v.stride_t, tiles.key(i) + x * 16, w.n_k, lane, lds + (buffer * 2 + 1) * kTileBytes + x * 16 * kRowBytes);
+            keys.copy(w.n_k, 16, lane, lds + buffer * 2 * kTileBytes + x * 16 * kRowBytes);
+            values.copy(w.n_k, 16, lane, lds + (buffer * 2 + 1) * kTileBytes + x * 16 * kRowBytes);
         }
     };
     int buffer = 0;
@@ -480,10 +508,10 @@ size_t prompt_workspace_bytes(const PromptParams& p) {
 hipError_t launch_prompt_attention(const PromptParams& params, void* workspace, size_t workspace_bytes, hipStream_t stream) {
     Args p{};
     static_cast<PromptParams&>(p) = params;
-    // (the copies' lane offsets are 32 bits over four rows; rows are counted in 31 bits)
+    // (the copies' lane offsets are 32 bits over 16 rows; rows are counted in 31 bits)
     const int rep = p.n_q_heads / p.n_kv_heads;
     const int64_t rows = (int64_t)p.max_q * rep, pairs = (int64_t)p.batch * p.n_kv_heads;
-    if (p.k.stride_t >= 1 << 28 || p.v.stride_t >= 1 << 28 || rows > 0x3fffffff || pairs > 0x7fffffff) return hipErrorNotSupported;
+    if (p.k.stride_t >= 1 << 26 || p.v.stride_t >= 1 << 26 || rows > 0x3fffffff || pairs > 0x7fffffff) return hipErrorNotSupported;
     Plan plan = plan_of(p);
     if (!workspace || workspace_bytes < prompt_workspace_bytes(p)) plan.splits = 1;
     const int tile_rows = plan.small ? kWaveRows : kWaves * kWaveRows;
