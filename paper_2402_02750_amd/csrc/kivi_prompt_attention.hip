@@ -230,13 +230,16 @@ struct Rows {
                 }
         }
     }
-    __device__ __forceinline__ void raise(const float16v (&s)[KB]) {
+    // the largest logit of this lane's row in a tile
+    __device__ __forceinline__ float largest(const float16v (&s)[KB]) const {
         float mx = -INFINITY;
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
-        mx = max_halves(mx) * c;
+        return max_halves(mx) * c;
+    }
+    __device__ __forceinline__ void raise(float mx) {
         if (__any(mx > m + kSlack || (m == kNothing && mx > kNothing))) {
             const float mn = fmaxf(m, mx), f = __builtin_amdgcn_exp2f(m - mn);
             m = mn;
@@ -333,6 +336,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_tiles_kernel(Args p) {
         lds_barrier();
         r.logits(sm[0][0], lane, s);
     }
+    float mx = 0.f;
+    if (count > 0) {
+        r.mask(p, w, tiles.key(0), half, s);
+        mx = r.largest(s);
+    }
     // tile i, whose logits are there, and the next one's logits
     auto step = [&](int i, auto parity, const float16v (&now)[2], float16v (&then)[2]) {
         constexpr int B = decltype(parity)::value;
@@ -340,11 +348,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_tiles_kernel(Args p) {
         lds_barrier();                                             // everybody's, and nobody reads the other buffers any more
         if (i + 2 < count) copy_keys(i + 2, B);
         if (i + 1 < count) copy_values(i + 1, B ^ 1);
-        float16v x[2] = {now[0], now[1]};
-        r.mask(p, w, tiles.key(i), half, x);
-        r.raise(x);
+        r.raise(mx);
         r.logits(sm[B ^ 1][0], lane, then);                        // (after the last tile: of what the buffer holds, not used)
-        r.add(sm[B][1], lane, x);
+        r.add(sm[B][1], lane, now);
+        r.mask(p, w, tiles.key(i + 1), half, then);
+        mx = r.largest(then);
     };
     for (int i = 0; i < count; i += 2) {
         step(i, std::integral_constant<int, 0>{}, s, next);
@@ -404,7 +412,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void prompt_rows_kernel(Args p) {
         float16v s[1];
         r.logits(sm[wave][buffer][0], lane, s);
         r.mask(p, w, tiles.key(i), half, s);
-        r.raise(s);
+        r.raise(r.largest(s));
         r.add(sm[wave][buffer][1], lane, s);
         buffer ^= 1;
     }
