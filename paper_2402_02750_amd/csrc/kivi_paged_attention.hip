@@ -639,6 +639,19 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
     bool first_unit = true;
     int slot = 0;
     advance_copy();
+    // The instruction arbiter favours the oldest wavefront of a SIMD, so the workgroups of a compute unit would finish one after the other,
+    // the last one alone: a wavefront's priority falls with the share of its interval that is done.
+    const int quarter = (x1 - x0) >> 2;
+    int priority = 3, drop_at = x0 + quarter;
+    __builtin_amdgcn_s_setprio(3);
+    auto progress = [&](int x) {
+        if (x < drop_at || priority == 0) return;
+        --priority;
+        drop_at += quarter;
+        if (priority == 2) __builtin_amdgcn_s_setprio(2);
+        else if (priority == 1) __builtin_amdgcn_s_setprio(1);
+        else __builtin_amdgcn_s_setprio(0);
+    };
     while (true) {
         const View& view = here.view;
         const int cost = view.cost(), kvh = here.unit / p.runs, h0 = (here.unit - kvh * p.runs) * p.run, live = min(p.run, rep - h0);
@@ -704,6 +717,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
         }
         const int j1 = records_to(here);
         for (int j = records_from(here); j < j1; ++j) {
+            progress(here.unit0 + rows_cost + j);
             wait_oldest();
             const int i = j * kWaves + wave;
             if (i < view.records && !((lost >> slot) & 1)) record_tile(&sm_ring[wave][slot][0], view, i < view.sink_records ? i : i + view.skip);
