@@ -153,6 +153,7 @@ __device__ __forceinline__ void wait_copies() {        // at most N vector-memor
 
 struct Args : PagedAttentionParams {
     int32_t runs, run;                 // runs of query heads per kv-head, heads of a run
+    FastDiv by_runs;
 };
 
 // What a sequence shows its newest token
@@ -165,9 +166,9 @@ struct View {
     int row_steps, steps;
     __device__ __forceinline__ int cost() const { return row_steps * kRowCost + steps; }
 };
-__device__ __forceinline__ View view_of(const Args& p, int length, int slot) {
+__device__ __forceinline__ View view_of(const Args& p, int length) {
     View v;
-    v.length = slot >= 0 && slot < p.max_sequences ? max(length, 0) : 0;
+    v.length = length;
     const int all = packed_records(v.length, p.residual);
     v.packed = min(all, p.max_pages << p.page_shift);                  // (records behind the table are masked)
     v.lowest = p.window > 0 ? max(v.length - p.window, 0) : 0;
@@ -183,6 +184,7 @@ __device__ __forceinline__ View view_of(const Args& p, int length, int slot) {
     v.row_tiles = (v.length - v.row0 + kTileTokens - 1) / kTileTokens;
     v.row_steps = (v.row_tiles + kWaves - 1) / kWaves;
     v.steps = (v.records + kWaves - 1) / kWaves;
+    if (v.row_steps + v.steps == 0) v.steps = 1;                       // (nothing of it is visible: its rows become 0)
     return v;
 }
 template <int BITS, int HP>
@@ -208,20 +210,26 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
 
     // ---- this workgroup's interval of the axis ----
     const int wg = ((int)blockIdx.x & 7) * (kWorkgroups / 8) + ((int)blockIdx.x >> 3);      // neighbours on the axis share a die
-    auto cost_of = [&](int b) { return b < p.batch ? view_of(p, p.lengths[b], p.slots ? p.slots[b] : b).cost() : 0; };
+    // (a sequence without tokens or with a slot outside the cache: 0)
+    auto length_of = [&](int b) {
+        const int slot = p.slots ? p.slots[b] : b;
+        return slot >= 0 && slot < p.max_sequences ? max(p.lengths[b], 0) : 0;
+    };
+    auto cost_of = [&](int tokens) { return tokens > 0 ? view_of(p, tokens).cost() : 0; };
     auto sum_all = [&](int x) { return __builtin_amdgcn_readlane(sum_upto(x), 63); };
-    int costs[kScanned];                                               // of the first sequences, 64 at a time
+    int tokens[kScanned], costs[kScanned];                             // of the first sequences, 64 at a time
     int total = 0, units = 0;
 #pragma unroll
     for (int i = 0; i < kScanned; ++i) {
-        costs[i] = 0;
+        tokens[i] = costs[i] = 0;
         if (i * 64 < p.batch) {
-            costs[i] = cost_of(i * 64 + lane);
+            if (i * 64 + lane < p.batch) tokens[i] = length_of(i * 64 + lane);
+            costs[i] = cost_of(tokens[i]);
             total += sum_all(costs[i]) * units_per_sequence;
             units += __popcll(__ballot(costs[i] > 0)) * units_per_sequence;
         }
     }
-    for (int b0 = kScanned * 64; b0 < p.batch; b0 += 64) total += sum_all(cost_of(b0 + lane)) * units_per_sequence;
+    for (int b0 = kScanned * 64; b0 < p.batch; b0 += 64) total += sum_all(b0 + lane < p.batch ? cost_of(length_of(b0 + lane)) : 0) * units_per_sequence;
     if (total == 0) return;
     // An interval of `length` of the axis for every workgroup, or, where that costs little more, every unit cut evenly on its own: `length`
     // is then the longest piece, and no workgroup enters two units.
@@ -249,26 +257,31 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
     // what of the axis is in front of a sequence: workgroups with pieces of their own, cost otherwise
     auto share_of = [&](int cost) { return (own_pieces ? (cost + length - 1) / length : cost) * units_per_sequence; };
     const int x_first = own_pieces ? wg : wg * length;
-    int b = -1, before = 0;                                            // the sequence of this workgroup's first unit, and where it begins
+    int b = -1, before = 0, n_tokens = 0;                              // the sequence of this workgroup's first unit, and where it begins
     {
         int sum = 0;
-        auto look = [&](int b0, int cost) {
+        auto look = [&](int b0, int length, int cost) {
             const int mine = share_of(cost), upto = sum_upto(mine);
             const uint64_t here = __ballot(sum + upto > x_first);
             if (here) {
                 const int at = __builtin_ctzll(here);
                 b = b0 + at;
                 before = sum + __builtin_amdgcn_readlane(upto - mine, at);
+                n_tokens = __builtin_amdgcn_readlane(length, at);
             }
             sum += __builtin_amdgcn_readlane(upto, 63);
         };
 #pragma unroll
         for (int i = 0; i < kScanned; ++i)
-            if (b < 0 && i * 64 < p.batch) look(i * 64, costs[i]);
-        for (int b0 = kScanned * 64; b < 0 && b0 < p.batch; b0 += 64) look(b0, cost_of(b0 + lane));
+            if (b < 0 && i * 64 < p.batch) look(i * 64, tokens[i], costs[i]);
+        for (int b0 = kScanned * 64; b < 0 && b0 < p.batch; b0 += 64) {
+            const int n = b0 + lane < p.batch ? length_of(b0 + lane) : 0;
+            look(b0, n, cost_of(n));
+        }
     }
     b = __builtin_amdgcn_readfirstlane(b);
     before = __builtin_amdgcn_readfirstlane(before);
+    n_tokens = __builtin_amdgcn_readfirstlane(n_tokens);
     if (b < 0) return;                                                 // (more workgroups than pieces, or than intervals)
     // A place on the axis: sequence, unit in it, and where the unit begins
     struct Place { int b, unit, unit0; View view; };
@@ -276,15 +289,18 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
         u.unit0 += u.view.cost();
         if (++u.unit == units_per_sequence) {
             u.unit = 0;
+            int n, slot;
             do {
                 ++u.b;
-                u.view = view_of(p, scalar(p.lengths, u.b), p.slots ? scalar(p.slots, u.b) : u.b);
-            } while (u.view.cost() == 0);
+                n = scalar(p.lengths, u.b);
+                slot = p.slots ? scalar(p.slots, u.b) : u.b;
+            } while (n <= 0 || slot < 0 || slot >= p.max_sequences);
+            u.view = view_of(p, n);
         }
     };
     Place here;
     here.b = b;
-    here.view = view_of(p, scalar(p.lengths, here.b), p.slots ? scalar(p.slots, here.b) : here.b);
+    here.view = view_of(p, n_tokens);
     int x0, x1, pieces = 1, piece = 0;                                 // the interval; own pieces: of the unit
     {
         const int cost = here.view.cost();
@@ -304,34 +320,49 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
     }
     // its steps of records in this interval: [first, end)
     auto records_from = [&](const Place& u) { return max(x0 - u.unit0 - u.view.row_steps * kRowCost, 0); };
-    auto records_to = [&](const Place& u) { return max(min(x1 - u.unit0, u.view.cost()) - u.view.row_steps * kRowCost, 0); };
+    auto records_to = [&](const Place& u) { return u.view.records > 0 ? max(min(x1 - u.unit0, u.view.cost()) - u.view.row_steps * kRowCost, 0) : 0; };
 
     // ---- copies of records into this wavefront's ring, NB ahead ----
     const uint32_t ring_lds = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)&sm_ring[wave][0][0]);
     const uint32_t lane16 = lane * 16;
     Place cursor = here;
-    int c_step = records_from(cursor), c_end = records_to(cursor), c_slot = 0, in_flight = 0;
+    // of the cursor's unit: row of the page table, the kv-head's records of page 0, this wavefront's next record, the last record, steps left
+    const int32_t* c_table;
+    const char* c_base;
+    int c_record, c_last, c_left;
+    const int64_t page_bytes = ((int64_t)p.n_kv_heads << p.page_shift) * kRecord;
+    auto enter_unit = [&](int first) {
+        c_table = p.page_table + cursor.b * p.page_table_stride;
+        c_base = p.pages + ((int64_t)p.by_runs.of(cursor.unit) << p.page_shift) * kRecord;
+        c_record = first * kWaves + wave;
+        c_last = cursor.view.records - 1;
+        c_left = records_to(cursor) - first;
+    };
+    enter_unit(records_from(cursor));
+    int c_slot = 0, in_flight = 0;
     uint32_t lost = 0;                                                 // slots whose record has no page
     auto advance_copy = [&]() {
-        while (c_step >= c_end) {
+        while (c_left <= 0) {
             if (cursor.unit0 + cursor.view.cost() >= x1) return;
             next_unit(cursor);
-            c_step = 0;
-            c_end = records_to(cursor);
+            enter_unit(0);
         }
-        const int i = min(c_step * kWaves + wave, cursor.view.records - 1);     // (no record for this wavefront: any)
+        const int i = min(c_record, c_last);                           // (no record for this wavefront: any)
         const int r = i < cursor.view.sink_records ? i : i + cursor.view.skip;
-        int page = scalar(p.page_table, cursor.b * p.page_table_stride + (r >> p.page_shift));
-        const bool bad = page < 0 || page >= p.n_pages;
-        lost = (lost & ~(1u << c_slot)) | (bad ? 1u << c_slot : 0u);
-        if (bad) page = 0;
-        const int kvh = cursor.unit / p.runs;
-        const char* rec = p.pages + (((((int64_t)page * p.n_kv_heads + kvh) << p.page_shift) + (r & ((1 << p.page_shift) - 1))) * kRecord);
+        int page = scalar(c_table, r >> p.page_shift);
+        c_record += kWaves;
+        --c_left;
+        const uint32_t bit = 1u << c_slot;
+        lost &= ~bit;
+        if ((uint32_t)page >= (uint32_t)p.n_pages) {
+            page = 0;
+            lost |= bit;
+        }
+        const char* rec = c_base + page * page_bytes + (r & ((1 << p.page_shift) - 1)) * kRecord;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");             // the slot's last readers have their data
 #pragma unroll
         for (int j = 0; j < NI; ++j) copy_to_lds(rec + j * 1024, lane16, ring_lds + c_slot * kRecord + j * 1024);
         c_slot = c_slot + 1 == NB ? 0 : c_slot + 1;
-        ++c_step;
         ++in_flight;
     };
     auto wait_oldest = [&]() {
@@ -361,8 +392,8 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
         const bool on = mx > 0.f;
         const int a = on ? min(kQueryExp + 127 - (int)(__float_as_uint(mx) >> 23), 28) : 0, a1 = a / 2;
         const _Float16 up1 = on ? (_Float16)__uint_as_float((uint32_t)(127 + a1) << 23) : (_Float16)0.f;
-        const _Float16 up2 = (_Float16)__uint_as_float((uint32_t)(127 + a - a1) << 23);
-        c_zero = p.softmax_scale * kLog2e * __uint_as_float((uint32_t)(127 - a) << 23);
+        const _Float16 up2 = (_Float16)__uint_as_float((uint32_t)(127 + a - a1) << 23 | (p.softmax_scale < 0.f ? 0x80000000u : 0u));
+        c_zero = fmaxf(fabsf(p.softmax_scale) * kLog2e, 1e-30f) * __uint_as_float((uint32_t)(127 - a) << 23);      // (not 0: masked logits stay -inf)
         c_code = c_zero * kKeyUnscale;
 #pragma unroll
         for (int cb = 0; cb < 4; ++cb) {
@@ -391,16 +422,11 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
     };
     // Probabilities 2^(prob_exp + logit - m) of this lane's four tokens, logit = x cx + zk; raises the maximum, and rescales the state by
     // rescale(factor), when a logit passes it by the slack
-    auto softmax = [&](const float (&x)[4], float cx, float zk, uint32_t live, float (&pv)[4], auto&& rescale) {
+    auto softmax = [&](const float (&x)[4], float cx, float zk, float (&pv)[4], auto&& rescale) {
         auto logits = [&](float off) {
-            float mx = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                pv[i] = fmaf(x[i], cx, off);
-                if (!((live >> i) & 1)) pv[i] = -INFINITY;
-                mx = fmaxf(mx, pv[i]);
-            }
-            return mx;
+            for (int i = 0; i < 4; ++i) pv[i] = fmaf(x[i], cx, off);
+            return fmaxf(fmaxf(pv[0], pv[1]), fmaxf(pv[2], pv[3]));
         };
         const float mx = logits(zk - (m - prob_exp));
         if (__any(mx > prob_exp + kSlack)) {
@@ -448,17 +474,13 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
         exchange(fa);
         exchange(fb);
     };
-    // which of this lane's tokens of a tile that begins with token t0 are visible
-    auto live_of = [&](const View& v, int t0) -> uint32_t {
-        uint32_t live = 0xF;
-        if (t0 < v.lowest || t0 + kTileTokens > v.length) {
+    // masks this lane's tokens of a tile that begins with token t0 (their factor is positive)
+    auto mask = [&](const View& v, int t0, float (&x)[4]) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int t = t0 + tok + i;
-                if (t >= v.length || (t < v.lowest && t >= v.sinks)) live &= ~(1u << i);
-            }
+        for (int i = 0; i < 4; ++i) {
+            const int t = t0 + tok + i;
+            x[i] = (t < v.length) & ((t >= v.lowest) | (t < v.sinks)) ? x[i] : -INFINITY;
         }
-        return live;
     };
     auto any_above = [&](const unsigned char* scales, uint32_t limit) -> bool {      // of 128 scales, two per lane
         typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
@@ -532,7 +554,8 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
             l *= f;
             prob_exp = -(float)kSlack;
         }
-        softmax(x, big ? c_code * (float)(1 << kKeyScaleShift) : c_code, dz[0] * c_zero, live_of(v, r * kTileTokens), pv, rescale_acc);
+        if (r * kTileTokens < v.lowest) mask(v, r * kTileTokens, x);
+        softmax(x, big ? c_code * (float)(1 << kKeyScaleShift) : c_code, dz[0] * c_zero, pv, rescale_acc);
         // outputs: this lane's tokens 8 kb .. 8 kb + 7, as pairs, of a channel group
         Frag fa, fb, z;
         split(pv, fa, fb);
@@ -619,7 +642,8 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
         float x[4], pv[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) x[k] = is_lo ? d[1][k] : d[0][k];
-        softmax(x, c_zero, 0.f, live_of(v, t0), pv, [&](float f) {
+        if (t0 < v.lowest || t0 + kTileTokens > v.length) mask(v, t0, x);
+        softmax(x, c_zero, 0.f, pv, [&](float f) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) ro[e] *= f;
         });
@@ -654,7 +678,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
     };
     while (true) {
         const View& view = here.view;
-        const int cost = view.cost(), kvh = here.unit / p.runs, h0 = (here.unit - kvh * p.runs) * p.run, live = min(p.run, rep - h0);
+        const int cost = view.cost(), kvh = p.by_runs.of(here.unit), h0 = (here.unit - kvh * p.runs) * p.run, live = min(p.run, rep - h0);
         const int64_t q_row = (int64_t)here.b * p.n_q_heads + kvh * rep + h0;
         {
             Frag raw[4];
@@ -840,6 +864,7 @@ hipError_t launch_paged_attention(const PagedAttentionParams& params, hipStream_
     const int rep = p.n_q_heads / p.n_kv_heads;
     p.runs = (rep + kMaxHeads - 1) / kMaxHeads;
     p.run = (rep + p.runs - 1) / p.runs;
+    p.by_runs = FastDiv::by(p.runs);
     // (the axis has to fit 31 bits)
     const int64_t records = (int64_t)p.max_pages << p.page_shift, rows = (p.residual + 2 * kTileTokens) / kTileTokens;
     const int64_t cost = (records + kWaves - 1) / kWaves + ((rows + kWaves - 1) / kWaves) * kRowCost;

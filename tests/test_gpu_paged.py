@@ -225,6 +225,24 @@ def test_empty_and_invalid_sequences():
     assert all(torch.equal(a, b) for a, b in zip(before, run.cache.buffers.values()))      # (sequence 0's slot is -1)
 
 
+def test_sequences_of_which_nothing_is_visible():
+    """No fp16 rows (R = 0) and no pages: rows of 0, between sequences that have some."""
+    torch = gh.require_gpu()
+    run = Run(5, 4, 2, 2, residual=0, most=320)
+    run.append([64, 33, 320, 32, 100])
+    run.check_cache()
+    run.attention()
+    none = run.table.clone()
+    none[[0, 2, 3]] = -1
+    q = torch.randn(5, 4, 128, device="cuda").half()
+    for table in (none, none[:, :0]):
+        out = torch.full((5, 4, 128), 9.0, dtype=torch.float16, device="cuda")
+        kivi.kivi_paged_attention(run.cache, kivi.PagedBatch(table, run.lengths), q, 0.1, out)
+        torch.cuda.synchronize()
+        assert (out[[0, 2, 3]] == 0).all() and torch.isfinite(out).all()
+        assert not (out[[1, 4]] == 0).all(-1).any()
+
+
 def test_two_rows_of_one_sequence_and_prefix_pages():
     """Attention may read one sequence twice, and pages that two sequences share."""
     torch = gh.require_gpu()
