@@ -455,7 +455,7 @@ typedef struct kivi_paged_layout {
     int32_t residual;           /* R, a multiple of 32                                                 */
     int32_t page_tokens;        /* a power of two, 32 to 4096                                          */
     int32_t n_pages;
-    int32_t cap_r_tokens;       /* a multiple of 32, >= R + 32                                         */
+    int32_t cap_r_tokens;       /* a multiple of 32, R + 32 to 2^20                                    */
 } kivi_paged_layout_t;
 
 typedef struct kivi_paged_cache {

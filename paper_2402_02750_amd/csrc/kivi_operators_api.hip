@@ -65,7 +65,7 @@ int check_paged_layout(const kivi_paged_layout_t* l) {
     if (l->head_dim != kHeadDim || (l->bits != 2 && l->bits != 4) || l->group != kTileTokens) return KIVI_ERR_UNSUPPORTED;
     if (l->residual % kTileTokens != 0 || l->cap_r_tokens % kTileTokens != 0 || l->cap_r_tokens < (int64_t)l->residual + kTileTokens) return KIVI_ERR_INVALID_ARG;
     if (l->page_tokens < kTileTokens || l->page_tokens > 4096 || (l->page_tokens & (l->page_tokens - 1))) return KIVI_ERR_INVALID_ARG;
-    if (l->n_q_heads / l->n_kv_heads > kMaxRepTotal) return KIVI_ERR_UNSUPPORTED;
+    if (l->n_q_heads / l->n_kv_heads > kMaxRepTotal || l->cap_r_tokens > 1 << 20) return KIVI_ERR_UNSUPPORTED;
     return KIVI_OK;
 }
 int check_paged(const kivi_paged_layout_t* l, const kivi_paged_cache_t* c, const kivi_paged_batch_t* b) {

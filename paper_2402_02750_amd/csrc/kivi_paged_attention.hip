@@ -868,7 +868,7 @@ hipError_t launch_paged_attention(const PagedAttentionParams& params, hipStream_
     // (the axis has to fit 31 bits)
     const int64_t records = (int64_t)p.max_pages << p.page_shift, rows = (p.residual + 2 * kTileTokens) / kTileTokens;
     const int64_t cost = (records + kWaves - 1) / kWaves + ((rows + kWaves - 1) / kWaves) * kRowCost;
-    if (cost * p.batch * p.n_kv_heads * p.runs > 0x40000000) return hipErrorNotSupported;
+    if (cost > 0x200000 || cost * p.batch * p.n_kv_heads * p.runs > 0x40000000) return hipErrorNotSupported;
     char* ws = reinterpret_cast<char*>(p.counters);
     p.part_o = reinterpret_cast<float*>(ws + kWorkgroups * sizeof(int32_t));
     p.part_ml = p.part_o + (size_t)kWorkgroups * 2 * kMaxHeads * kPartFloats;

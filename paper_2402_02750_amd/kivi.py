@@ -527,9 +527,8 @@ def kivi_prompt_attention(q, k, v, out, softmax_scale, q_starts=None, k_starts=N
     workspace = None
     if need.value:
         import torch
-        workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-        if stream is not None:
-            workspace.record_stream(stream)
+        with torch.cuda.stream(stream):                 # (the allocator orders its reuse by this stream)
+            workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
     _check(lib.kivi_prompt_attention(p, *[_ONE_TENSOR.pack(*t) for t in tensors], workspace.data_ptr() if need.value else None, need.value,
                                      _stream_handle(stream)), "kivi_prompt_attention")
     return out

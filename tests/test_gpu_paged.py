@@ -177,6 +177,24 @@ def test_steps_with_rotation(bits, q_heads, kv_heads, rotary, interleaved, bf16)
     run.attention(window=77, sinks=5)
 
 
+@pytest.mark.parametrize("bits,q_heads,kv_heads", [(2, 71, 1), (4, 128, 1), (2, 20, 2)])
+def test_wide_groups(bits, q_heads, kv_heads):
+    """More query heads per kv-head than a unit has: runs of them."""
+    print(f"case paged wide groups {q_heads}/{kv_heads} bits={bits}", flush=True)
+    run = Run(3, q_heads, kv_heads, bits)
+    run.append([40, 500, 161])
+    run.attention()
+    run.attention(window=120, sinks=3)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.05])
+def test_softmax_scales(scale):
+    run = Run(2, 6, 2, 2)
+    run.append([400, 70])
+    run.attention(scale=scale)
+    run.attention(scale=scale, window=100, sinks=33)
+
+
 def test_larger_rings_and_slots():
     """A ring with room to spare (a chunk is one launch then), rows of the batch in other slots, a batch smaller than the cache."""
     run = Run(3, 4, 2, 2, cap_r=256, slots=[6, 0, 3])

@@ -137,7 +137,7 @@ def test_paged_sizes(lib):
     (dict(max_sequences=0), INVALID), (dict(n_q_heads=7), INVALID), (dict(n_q_heads=258), UNSUPPORTED), (dict(head_dim=64), UNSUPPORTED), (dict(bits=8), UNSUPPORTED),
     (dict(group=64), UNSUPPORTED), (dict(residual=48), INVALID), (dict(residual=-32), INVALID), (dict(page_tokens=48), INVALID),
     (dict(page_tokens=16), INVALID), (dict(page_tokens=8192), INVALID), (dict(n_pages=0), INVALID), (dict(cap_r_tokens=64), INVALID),
-    (dict(cap_r_tokens=100), INVALID),
+    (dict(cap_r_tokens=100), INVALID), (dict(cap_r_tokens=(1 << 20) + 32), UNSUPPORTED),
 ])
 def test_bad_paged_layouts(lib, kw, status):
     l = _layout(**kw)
