@@ -418,6 +418,7 @@ _ONE_TENSOR = struct.Struct(_TENSOR)
 _PROMPT = struct.Struct("iiiiiii4xPPiiiif4x")
 _ROWS = struct.Struct(_TENSOR * 4 + "iii4xPP")
 _QUERY = struct.Struct("PPiiif")
+_ROTATION = struct.Struct("PPiii4x")
 
 
 def _type_of(x) -> int:
@@ -465,6 +466,7 @@ class Rotation:
         assert table.dim() == 2 and table.dtype == torch.float32 and table.is_contiguous(), "expected a contiguous fp32 table"
         self.table = table
         self.interleaved = int(interleaved)
+        self._fields = table.data_ptr(), *table.shape, self.interleaved
         self._alone = self.c()
 
     def c(self, positions=None, rows=0) -> kivi_rotation_t:
@@ -496,7 +498,7 @@ def kivi_norm_rotate(q, q_out, k=None, k_out=None, q_weight=None, k_weight=None,
     r = None
     if rotation is not None:
         assert positions is not None, "a rotation needs positions"
-        r = ctypes.byref(rotation.c(positions, rows))
+        r = _ROTATION.pack(rotation._fields[0], _int32(positions, rows) or 0, *rotation._fields[1:])
     _check(load_library().kivi_norm_rotate(jobs, n, rows, eps, r, _stream_handle(stream)), "kivi_norm_rotate")
 
 
