@@ -497,7 +497,8 @@ int kivi_paged_sizes(const kivi_paged_layout_t* layout, kivi_paged_sizes_t* size
  * Append the new tokens of every sequence to the paged cache: rotate keys (and queries) on the way, quantise the
  * groups that leave the window (Section 3.3, formula of Section 3.1, the contract above) out of the fp16 rows or straight out of
  * the new ones, and store the rows that stay.  lengths[b] counts the new tokens already.  Keys are rotated in fp32, each
- * product and the difference rounded on its own, and rounded to fp16 once; these fp16 numbers are what is quantised.
+ * product and the difference rounded on its own, and rounded to fp16 once; these fp16 numbers are what is quantised.  (bf16 numbers
+ * that fp16 does not hold are outside the contract, as numbers that are not finite.)
  *   A sequence whose rows are outside [0, n_rows), whose count of them is negative, above max_new or above lengths[b], or whose slot
  *   is outside [0, max_sequences), is left as it is, its queries too.  Groups whose page is outside the table or [0, n_pages) are not
  *   stored.  No two sequences of a call may share a slot or a page that is written.
@@ -521,7 +522,8 @@ typedef struct kivi_paged_query {
  * kivi_decode_attention, for sequences of any lengths in one launch that divides the visible records evenly over
  * the device.
  *   workspace   device scratch of kivi_paged_sizes' bytes, zero-filled once before its first use; every call
- *               leaves it ready for the next one.  Calls that overlap (two streams, two graphs) must not share it.
+ *               leaves it ready for the next one.  Calls that overlap (two streams, two graphs) must not share it, and lengths,
+ *               slots and pages must not change while a call runs.
  * Rows of `out` of sequences with lengths[b] < 1 or a slot outside [0, max_sequences) are left as they are.  Records whose
  * page is outside the table or [0, n_pages) count as masked; a row that sees nothing at all becomes 0.
  * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.

@@ -55,7 +55,8 @@ PromptParams prompt_params(const kivi_prompt_t* p) {
     r.q_starts = p->q_starts; r.k_starts = p->k_starts;
     r.batch = p->batch; r.n_q_heads = p->n_q_heads; r.n_kv_heads = p->n_kv_heads; r.bf16 = p->type == KIVI_TYPE_BF16;
     r.max_q = p->max_q; r.max_k = p->max_k; r.q_rows = p->q_rows; r.k_rows = p->k_rows;
-    r.window = p->window; r.sinks = p->sinks; r.softmax_scale = p->softmax_scale;
+    r.window = p->window < p->max_k ? p->window : 0;       // (one that no sequence is longer than hides nothing)
+    r.sinks = p->sinks; r.softmax_scale = p->softmax_scale;
     return r;
 }
 

@@ -12,6 +12,10 @@
 // the rows are a launch after the groups.  (One wavefront for the groups that read slots and the rows that replace them, all in one launch: its
 // registers slowed the groups down, 16 x 4096 tokens, 32 heads 305 us against 266.)
 //
+// Bound: memory for prompts (16 x 4096 tokens, 32 heads 264 us, 4.9 TB/s, as a copy; 16 of them are the rows' launch, which has 83 MB to move), the launch for
+// single tokens (32 heads 3.0 us, 64 sequences, 32 / 8 heads with queries 7).  Four tokens per wavefront of the rows: 267; rows of sequences that had
+// nothing before in the groups' launch: 272.
+//
 // The packed codes are a bit contract, so the rotation is one too: fp32 products and one difference, each rounded on its own
 // (this file is compiled without contraction), then one rounding to fp16.
 #include "kivi_paged.h"

@@ -2,18 +2,31 @@
 //
 // Work: a unit is (sequence, kv-head, run of up to eight query heads).  What a unit has to visit -- its visible records and tiles of 32
 // fp16 rows -- follows from the sequence's length, and is put on one axis for all units, in steps of one record or tile per
-// wavefront.  Every workgroup adds up the lengths by itself and takes one interval of the axis, so the device is divided
-// evenly whatever the lengths, and nothing but the batch's size is known to the host.  A unit that lies in one interval is written
-// out by it; of one that several share each leaves a part (maximum, sum, outputs) in the workspace, and the last to come joins them.
+// wavefront.  Every workgroup adds up the lengths by itself (sums across lanes without LDS) and takes one interval of the axis, so the
+// device is divided evenly whatever the lengths, and nothing but the batch's size is known to the host: a captured call follows lengths and
+// pages.  Where that leaves the longest piece little longer (few units, short ones), each unit is cut evenly on its own instead, and no workgroup
+// enters two: 8 sequences of 500 tokens, 32 / 8 heads 20.6 -> 13.2 us.  A unit that lies in one interval is written out by it; of one that several
+// share each leaves a part (maximum, sum, outputs) in the workspace, and the last to come joins them.  A workgroup shares its first and its
+// last unit at most, so the workspace has two parts per workgroup whatever the batch; a unit is counted where its first workgroup is.
 //
 // Products: 16x16x32 matrix instructions; operand rows are tokens (keys) and channels (values), columns are query heads.  Lane
 // (n = lane % 16, kb = lane / 16) makes the eight contraction elements 8 kb .. 8 kb + 7 of column n: head n % HP; n < 8: rounded products, n >= 8: what
-// the rounding left, so that a pair of columns together has 21 bits.  Codes are operands as they are, as subnormal fp16 numbers
-// (their place in the 16 bits is a power of two that goes into the other factor); scales go into the other operand:
+// the rounding left, so that a pair of columns together has 21 bits.  (Rounded products alone cost 2e-4 of the output, as much as its own rounding.)  Codes
+// are operands as they are, as subnormal fp16 numbers (their place in the 16 bits is a power of two that goes into the other factor); scales go into the
+// other operand:
 //   logit_t = sum_c code_tc (s_c q_c) + sum_c z_c q_c,     o_c = sum_t code_tc (p_t s_tg) + sum_t p_t z_tg
 // Queries enter times a power of two that puts the largest element into [2^8, 2^9), probabilities times 2^8 (4 bits: 2^11); tiles with
 // scales that could leave fp16's range with that (keys 2^6, values 2^3; 4 bits 2^0) take the scales 2^-9, or from then on the probabilities 2^-4.
 // The running maximum moves where a logit passes it by more than 2^4.
+//
+// A record is one contiguous piece of memory, so it takes three (4 bits: five) asynchronous copies of 1 KB into the wavefront's own ring in LDS,
+// NB records ahead, across unit borders, without barriers; the page number comes through the scalar cache.  fp16 rows are loaded straight into
+// registers: keys are operands as they are, value rows are turned by byte permutes.
+//
+// Bound: issue of vector instructions and memory, which overlap in part: of 64 sequences of 500-8000 tokens (32 / 8 heads, 2 bits, 257 MB) the copies
+// alone take 49 us, the arithmetic alone 46, both 62.5 (4.1 TB/s); 12 us of each are what a launch pays once (lengths, first page, first record: 5; leaving units,
+// counting, joining: 7).  16 x 32 767 tokens, 64 / 8 heads, 4 bits 121 us (5.6 TB/s); 32 x 16 001 tokens, 32 heads, window 4096 95 (4.9 TB/s);
+// one sequence of 3001 tokens, 32 heads 14.3.  Four wavefronts per SIMD (128 registers) spill: 64 -> 104 us; a ring of four records at 2 bits: no change.
 #include "kivi_paged.h"
 
 #include <algorithm>
@@ -285,23 +298,28 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
     if (b < 0) return;                                                 // (more workgroups than pieces, or than intervals)
     // A place on the axis: sequence, unit in it, and where the unit begins
     struct Place { int b, unit, unit0; View view; };
+    int x0, x1, pieces = 1, piece = 0;                                 // the interval; own pieces: of the unit
     auto next_unit = [&](Place& u) {                                   // (only where another one follows)
         u.unit0 += u.view.cost();
         if (++u.unit == units_per_sequence) {
             u.unit = 0;
-            int n, slot;
-            do {
-                ++u.b;
+            int n = 0, slot = -1;
+            while (++u.b < p.batch) {
                 n = scalar(p.lengths, u.b);
                 slot = p.slots ? scalar(p.slots, u.b) : u.b;
-            } while (n <= 0 || slot < 0 || slot >= p.max_sequences);
+                if (n > 0 && slot >= 0 && slot < p.max_sequences) break;
+            }
+            if (u.b >= p.batch) {                                      // (lengths that change under the call: it ends here)
+                u.b = p.batch - 1;
+                u.unit0 = x1;
+                n = 0;
+            }
             u.view = view_of(p, n);
         }
     };
     Place here;
     here.b = b;
     here.view = view_of(p, n_tokens);
-    int x0, x1, pieces = 1, piece = 0;                                 // the interval; own pieces: of the unit
     {
         const int cost = here.view.cost();
         if (own_pieces) {

@@ -17,6 +17,13 @@
 // Two kernels.  prompt_tiles_kernel: a workgroup has 128 rows and walks over tiles of 64 keys that its four wavefronts share.
 // prompt_rows_kernel, where those workgroups would not fill the device: 32 rows, the wavefronts take the tiles (of 32 keys) in turn, each with buffers
 // of its own and without barriers, and join in LDS; with a workspace, several workgroups share the keys of the same rows, and a second launch joins them.
+//
+// Tiles arrive by asynchronous copies into two buffers of keys and two of values, one tile ahead; the logits of the next tile are asked for before the
+// exponentials of this one, and its maximum before the barrier.  In LDS the 16-byte pieces of a row change place so that no read has bank conflicts.
+// Bound: the card's power.  4 x 4096 tokens, 32 / 8 heads, bf16 546 us, 1.01 PFLOP/s (a library product of 8192^3 1.19); on zeros instead of normal numbers it
+// runs in 414 us (the product: 1.76 PFLOP/s).  The clock is at 1.8 of 2.4 GHz, matrix instructions take half of the cycles, vector ones 40 %.  What did not help:
+// interleaving the two by hand (598-619 us), wavefront priorities (583-594), sums of probabilities by dot products (550), eight wavefronts per workgroup (559),
+// the workgroups of one pair after another (555).  8001 tokens, window 2048 and 4 first keys, fp16 263 us (0.89 PFLOP/s); 1001 tokens, 4 heads 14.8.
 #include "kivi_prompt.h"
 
 #include <algorithm>

@@ -592,6 +592,7 @@ class PagedBatch:
         import torch
         n = lengths.numel()
         assert page_table.dim() == 2 and page_table.shape[0] == n and page_table.dtype == torch.int32 and (page_table.shape[1] < 2 or page_table.stride(1) == 1)
+        assert n == 1 or page_table.stride(0) >= page_table.shape[1], "rows of the page table must not overlap"
         assert page_table.device == lengths.device and (slots is None or slots.device == lengths.device), "one device"
         self.page_table, self.lengths, self.slots = page_table, lengths, slots
         self.size = n

@@ -54,6 +54,9 @@ def _dtype(torch, name):
     (1, 2, 2, 40, 0, "fp16", 0, 0),             # no keys at all
     (3, 2, 2, 128, 128, "fp16", 0, 3),          # sinks without a window mean nothing
     (1, 71, 1, 70, 70, "fp16", 0, 0),
+    (1, 2, 2, 300, 40, "fp16", 2 ** 31 - 1, 2 ** 31 - 1),
+    (1, 4, 1, 90, 2300, "bf16", 700, 2 ** 31 - 1),      # sinks longer than everything
+    (9, 16, 8, 140, 140, "fp16", 64, 32),       # 128-row tiles, pairs per die
 ])
 def test_uniform_batches(batch, q_heads, kv_heads, n_q, n_k, dtype, window, sinks):
     torch = gh.require_gpu()

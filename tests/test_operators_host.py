@@ -227,3 +227,17 @@ def test_binding_refuses_other_devices(lib):
         assert kivi._type_of(torch.zeros(1, dtype=torch.bfloat16)) == kivi.KIVI_TYPE_BF16
         with pytest.raises(kivi.KiviError):
             kivi._type_of(torch.zeros(1))
+
+
+def test_page_tables_whose_rows_overlap_are_refused(lib):
+    torch = pytest.importorskip("torch")
+    lengths = torch.ones(3, dtype=torch.int32)
+    with pytest.raises(AssertionError):
+        kivi.PagedBatch(torch.zeros(1, 4, dtype=torch.int32).expand(3, 4), lengths)
+    with pytest.raises(AssertionError):
+        kivi.PagedBatch(torch.zeros(4, 3, dtype=torch.int32).t(), lengths)
+    with pytest.raises(AssertionError):
+        kivi.PagedBatch(torch.zeros(2, 4, dtype=torch.int32), lengths)
+    b = kivi.PagedBatch(torch.zeros(3, 8, dtype=torch.int32)[:, :4], lengths)
+    assert (b.c.batch, b.c.max_pages, b.c.page_table_stride) == (3, 4, 8)
+    assert kivi.PagedBatch(torch.zeros(1, 4, dtype=torch.int32).expand(1, 4), lengths[:1]).c.page_table_stride >= 4
