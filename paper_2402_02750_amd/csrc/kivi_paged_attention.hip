@@ -11,13 +11,14 @@
 //
 // Products: 16x16x32 matrix instructions; operand rows are tokens (keys) and channels (values), columns are query heads.  Lane
 // (n = lane % 16, kb = lane / 16) makes the eight contraction elements 8 kb .. 8 kb + 7 of column n: head n % HP; n < 8: rounded products, n >= 8: what
-// the rounding left, so that a pair of columns together has 21 bits.  (Rounded products alone cost 2e-4 of the output, as much as its own rounding.)  Codes
+// the rounding left, so that a pair of columns together has 21 bits.  (Rounded products alone: 2e-4 of the output by estimate, as much as its own rounding.)  Codes
 // are operands as they are, as subnormal fp16 numbers (their place in the 16 bits is a power of two that goes into the other factor); scales go into the
 // other operand:
 //   logit_t = sum_c code_tc (s_c q_c) + sum_c z_c q_c,     o_c = sum_t code_tc (p_t s_tg) + sum_t p_t z_tg
 // Queries enter times a power of two that puts the largest element into [2^8, 2^9), probabilities times 2^8 (4 bits: 2^11); tiles with
 // scales that could leave fp16's range with that (keys 2^6, values 2^3; 4 bits 2^0) take the scales 2^-9, or from then on the probabilities 2^-4.
-// The running maximum moves where a logit passes it by more than 2^4.
+// The running maximum moves where a logit passes it by more than 2^4.  One query head per kv-head (HP = 1) makes the same products in another
+// way, below at record_one: 32 x 16 001 tokens, window 4096 99 -> 82 us, 16 x 4096 53 -> 46, 4 bits 8 x 8191, 40 heads 79 -> 78.
 //
 // A record is one contiguous piece of memory, so it takes three (4 bits: five) asynchronous copies of 1 KB into the wavefront's own ring in LDS,
 // NB records ahead, across unit borders, without barriers; the page number comes through the scalar cache.  fp16 rows are loaded straight into
@@ -25,8 +26,9 @@
 //
 // Bound: issue of vector instructions and memory, which overlap in part: of 64 sequences of 500-8000 tokens (32 / 8 heads, 2 bits, 257 MB) the copies
 // alone take 49 us, the arithmetic alone 46, both 62.5 (4.1 TB/s); 12 us of each are what a launch pays once (lengths, first page, first record: 5; leaving units,
-// counting, joining: 7).  16 x 32 767 tokens, 64 / 8 heads, 4 bits 121 us (5.6 TB/s); 32 x 16 001 tokens, 32 heads, window 4096 95 (4.9 TB/s);
-// one sequence of 3001 tokens, 32 heads 14.3.  Four wavefronts per SIMD (128 registers) spill: 64 -> 104 us; a ring of four records at 2 bits: no change.
+// counting, joining: 7).  16 x 32 767 tokens, 64 / 8 heads, 4 bits 121 us (5.6 TB/s); 32 x 16 001 tokens, 32 heads, window 4096 82 (5.6 TB/s);
+// one sequence of 3001 tokens, 32 heads 14.3.  Four wavefronts per SIMD (128 registers) spill: 64 -> 104 us; a ring of four records at 2 bits, units counted
+// at the end of an interval, the first fp16 rows asked for with the query (spills): no gain.
 #include "kivi_paged.h"
 
 #include <algorithm>
@@ -97,6 +99,28 @@ __device__ __forceinline__ int sum_upto(int x) {
     x = add_from<0x118, 0xF>(x);
     x = add_from<0x142, 0xA>(x);       // the last of 16 to the next 16, the last of 32 to the next 32
     return add_from<0x143, 0xC>(x);
+}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141;
+__device__ __forceinline__ float wave_sum(float x) {
+    x += dpp<kXor1>(x);
+    x += dpp<kXor2>(x);
+    x += dpp<kHalfMirror>(x);
+    return add_rows(x + dpp<kRor8>(x));
+}
+__device__ __forceinline__ float wave_max(float x) {
+    x = fmaxf(x, dpp<kXor1>(x));
+    x = fmaxf(x, dpp<kXor2>(x));
+    x = fmaxf(x, dpp<kHalfMirror>(x));
+    return max_rows(fmaxf(x, dpp<kRor8>(x)));
+}
+// Products of two fp16 numbers with fp32 ones as x = hi + lo 2^-11.  a, b: the fp32 factors, a_up, b_up: 2^11 times those.
+constexpr float kLoMagnify = 2048.f, kLoShrink = 1.f / 2048.f;
+__device__ __forceinline__ void split_products(half2v s, float a, float b, float a_up, float b_up, half2v& hi, half2v& lo) {
+    // (fused operations with a zero, or with fp16 results: one mixed-precision instruction each)
+    hi = half2v{(_Float16)fmaf((float)s[0], a, 0.f), (_Float16)fmaf((float)s[1], b, 0.f)};
+    asm("" : "+v"(hi));                // (or its upper half is made twice)
+    lo = half2v{(_Float16)fmaf((float)hi[0], -kLoMagnify, fmaf((float)s[0], a_up, 0.f)),
+                (_Float16)fmaf((float)hi[1], -kLoMagnify, fmaf((float)s[1], b_up, 0.f))};
 }
 __device__ __forceinline__ half2v pack_rtz(float a, float b) { return __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(a, b)); }
 __device__ __forceinline__ float2 load_shared(const float* p) {      // of what another workgroup has stored
@@ -210,15 +234,18 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
     __shared__ __align__(16) unsigned char sm_ring[kWaves][NB][kRecord];
     __shared__ __align__(16) float sm_o[kWaves][HR][kHeadDim];
     __shared__ float sm_ml[kWaves][HP][2];
+    // HP = 1, operands of a record: key side rounded products (128), 16 halves of skew, remainders; value side 8 columns of 32 tokens
+    constexpr int kKeyColumn = 144, kOperandHalves = HP == 1 ? 272 : 8;
+    __shared__ __align__(16) _Float16 sm_operand[kWaves][kOperandHalves];
     __shared__ int sm_last;
-    static_assert(sizeof(sm_ring) + sizeof(sm_o) + sizeof(sm_ml) + 16 <= 160 * 1024 / 3 / 1280 * 1280, "three workgroups per compute unit");
+    static_assert(sizeof(sm_ring) + sizeof(sm_o) + sizeof(sm_ml) + sizeof(sm_operand) + 16 <= 160 * 1024 / 3 / 1280 * 1280, "three workgroups per compute unit");
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, kb = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool is_lo = n >= 8;
     const int head = n & (HP - 1);
     const int row_pos = (n & 3) | ((n >> 3) & 1) << 2 | ((n >> 2) & 1) << 3;        // operand row m holds token row_pos of its half
     const int tok0 = (kb & 1) * 8 + (kb >> 1) * 4, tok = tok0 + (is_lo ? 16 : 0);   // this lane's tokens: tok + i
-    const int my_group = HP == 2 ? (n >> 1) & 3 : HP == 4 ? (n >> 2) & 1 : 0;
+    const int my_group = HP == 1 ? (n & 1) * 2 + ((n >> 1) & 1) : HP == 2 ? (n >> 1) & 3 : HP == 4 ? (n >> 2) & 1 : 0;
     const int rep = p.n_q_heads / p.n_kv_heads, units_per_sequence = p.n_kv_heads * p.runs;
 
     // ---- this workgroup's interval of the axis ----
@@ -398,9 +425,16 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
     half2v q_zero[4];                  // HP < 8: q 2^a of channel block n / 4
     float c_code, c_zero;              // logit = code sum * c_code + zero sum * c_zero
     half2v rounded[4] = {};            // keys' products in the lo columns, 0 in the hi columns
+    // HP = 1: the token of every record, and the channel groups 2 own_pair, + 1, whose value operand this lane makes; log2 of the factor of that
+    // token's codes; this lane's channels 2 lane, + 1 of q 2^a over the codes' places, 2^11 times those, and as they are; sums of this lane's
+    // probabilities and zero-points
+    const int own_i = (n >> 1) & 3, own_pair = n & 1, own_tok = kb * 4 + own_i + (is_lo ? 16 : 0);
+    const float own_exp = BITS == 2 && (own_i & 2) ? 2.f : 0.f;
+    float own_q[2], own_q_up[2], l_own = 0.f, z_own[2] = {0.f, 0.f};
+    half2v own_qz;
     constexpr uint64_t kLoColumns = 0xFF00FF00FF00FF00ull;
 
-    auto set_query = [&](const half8 (&raw)[4]) {
+    auto set_query = [&](const half8 (&raw)[4], half2v own) {
         float mx = 0.f;
 #pragma unroll
         for (int cb = 0; cb < 4; ++cb)
@@ -424,7 +458,16 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
                 qk[cb][r] = qz[cb][r] * half2v{pf, pf};
             }
         }
-        if constexpr (HP < 8) {
+        if constexpr (HP == 1) {
+            own_qz = own * half2v{up1, up1} * half2v{up2, up2};
+            const float place = __uint_as_float((uint32_t)(127 - (BITS == 2 ? 2 * (lane & 3) : 4 * (lane & 1))) << 23);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                own_q[i] = (float)own_qz[i] * place;
+                own_q_up[i] = own_q[i] * kLoMagnify;
+            }
+        }
+        if constexpr (HP > 1 && HP < 8) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const half2v even = is_lo ? qz[2][r] : qz[0][r], odd = is_lo ? qz[3][r] : qz[1][r];
@@ -464,6 +507,11 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
 #pragma unroll
         for (int u = 0; u < 8; ++u) acc[u] *= f;
         zsum *= f;
+        if constexpr (HP == 1) {
+            z_own[0] *= f;
+            z_own[1] *= f;
+            l_own *= f;
+        }
     };
     // fb: rounded (hi columns) or the remainder (lo columns), fa: the rounded ones in the lo columns, 0 in the others;
     // lane kb gets tokens 8 kb .. 8 kb + 7
@@ -497,142 +545,225 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = t0 + tok + i;
-            x[i] = (t < v.length) & ((t >= v.lowest) | (t < v.sinks)) ? x[i] : -INFINITY;
+            x[i] = ((t < v.length) & ((t >= v.lowest) | (t < v.sinks))) ? x[i] : -INFINITY;
         }
     };
-    auto any_above = [&](const unsigned char* scales, uint32_t limit) -> bool {      // of 128 scales, two per lane
+    auto any_above = [&](uint32_t s2, uint32_t limit) -> bool {                      // of 128 scales, two per lane
         typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
-        const uint32_t s2 = *reinterpret_cast<const uint32_t*>(scales + lane * 4), l2 = limit | limit << 16;
+        const uint32_t l2 = limit | limit << 16;
         return __any(__builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, s2), __builtin_bit_cast(ushort2v, l2))) != l2);
     };
 
     // ---- one record out of an LDS slot ----
-    auto record_tile = [&](const unsigned char* sl, const View& v, int r) {
-        uint32_t w[2 * BITS];
+    // HP = 1: with one head the columns would be copies of each other if every lane made its own.  Instead a lane makes two elements of the key
+    // operand (two channels) and of the value operand (one token, two channel groups), which fill the columns through LDS, and its softmax work is one token.
+    auto record_one = [&](const unsigned char* sl, const View& v, int r) {
+        if constexpr (HP == 1) {
+            const unsigned char* scales = sl + kScaleOff;
+            const uint32_t k_scale = *reinterpret_cast<const uint32_t*>(scales + lane * 4), k_zero = *reinterpret_cast<const uint32_t*>(scales + 256 + lane * 4);
+            const uint32_t v_scale = *reinterpret_cast<const uint32_t*>(scales + 512 + own_tok * 8 + own_pair * 4), v_zero = *reinterpret_cast<const uint32_t*>(scales + 768 + own_tok * 8 + own_pair * 4);
+            uint32_t kw[2 * BITS], vw[2 * BITS];
 #pragma unroll
-        for (int pl = 0; pl < kPlanes; ++pl) {
-            const uint4v q4 = *reinterpret_cast<const uint4v*>(sl + pl * 1024 + (kb * 16 + row_pos) * 16);
+            for (int pl = 0; pl < kPlanes; ++pl) {
+                const uint4v a = *reinterpret_cast<const uint4v*>(sl + pl * 1024 + lane16), b = *reinterpret_cast<const uint4v*>(sl + kScaleOff + 1024 + pl * 1024 + lane16);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) w[4 * pl + k] = q4[k];
-        }
-        const bool big = any_above(sl + kScaleOff, kKeyScaleLimit);
-        float4v d0 = {0.f, 0.f, 0.f, 0.f}, d1 = d0, dz = d0;
-        Frag s[4];
-#pragma unroll
-        for (int cb = 0; cb < 4; ++cb) {
-            s[cb].v = *reinterpret_cast<const uint4v*>(sl + kScaleOff + cb * 64 + kb * 16);
-            if constexpr (HP >= 8) {
-                Frag z;
-                z.v = *reinterpret_cast<const uint4v*>(sl + kScaleOff + 256 + cb * 64 + kb * 16);
-                dz = __builtin_amdgcn_mfma_f32_16x16x32_f16(z.h, query_frag(cb), dz, 0, 0, 0);
-            }
-        }
-        if constexpr (HP < 8) {
-            // (eight channels in each of the four columns that share a head and kb)
-            Frag z;
-            z.v = *reinterpret_cast<const uint4v*>(sl + kScaleOff + 256 + (n >> 2) * 64 + kb * 16);
-            float sum = 0.f;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) sum = __builtin_amdgcn_fdot2(q_zero[k], z.p[k], sum, false);
-            sum += dpp<kRor8>(sum);
-            sum += dpp<kRor4>(sum);
-            dz[0] = add_rows(sum);
-        }
-        if (big) {
-            const half2v f = {(_Float16)(1.f / (1 << kKeyScaleShift)), (_Float16)(1.f / (1 << kKeyScaleShift))};
-#pragma unroll
-            for (int cb = 0; cb < 4; ++cb)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) s[cb].p[k] *= f;
-        }
-#pragma unroll
-        for (int cb = 0; cb < 4; ++cb) {
-            Frag f;
-            // in the lo columns alone; the hi columns' zeros stay
-            uint64_t active;
-            asm("s_and_saveexec_b64 %4, %13\n\tv_pk_mul_f16 %0, %5, %9\n\tv_pk_mul_f16 %1, %6, %10\n\tv_pk_mul_f16 %2, %7, %11\n\tv_pk_mul_f16 %3, %8, %12\n\ts_mov_b64 exec, %4"
-                : "+&v"(rounded[0]), "+&v"(rounded[1]), "+&v"(rounded[2]), "+&v"(rounded[3]), "=&s"(active)
-                : "v"(qk[cb][0]), "v"(qk[cb][1]), "v"(qk[cb][2]), "v"(qk[cb][3]), "v"(s[cb].p[0]), "v"(s[cb].p[1]), "v"(s[cb].p[2]), "v"(s[cb].p[3]), "s"(kLoColumns)
-                : "scc");
-#pragma unroll
-            for (int k = 0; k < 4; ++k) f.p[k] = __builtin_elementwise_fma(qk[cb][k], s[cb].p[k], -rounded[k]);
-            d0 = __builtin_amdgcn_mfma_f32_16x16x32_f16(key_fragment<BITS>(w, cb, 0), f.h, d0, 0, 0, 0);
-            d1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(key_fragment<BITS>(w, cb, 1), f.h, d1, 0, 0, 0);
-        }
-        float x[4], pv[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            // hi and lo column of a head share its tokens: hi columns take tok0 + k, lo columns 16 + tok0 + k
-            x[k] = is_lo ? d1[k] : d0[k];
-            x[k] += dpp<kRor8>(is_lo ? d0[k] : d1[k]);
-        }
-        if (prob_exp > 0.f && any_above(sl + kScaleOff + 512, kValueScaleLimit<BITS>)) {
-            const float f = __builtin_amdgcn_exp2f(-(float)kSlack - prob_exp);
-            rescale_acc(f);
-            l *= f;
-            prob_exp = -(float)kSlack;
-        }
-        if (r * kTileTokens < v.lowest) mask(v, r * kTileTokens, x);
-        softmax(x, big ? c_code * (float)(1 << kKeyScaleShift) : c_code, dz[0] * c_zero, pv, rescale_acc);
-        // outputs: this lane's tokens 8 kb .. 8 kb + 7, as pairs, of a channel group
-        Frag fa, fb, z;
-        split(pv, fa, fb);
-        const unsigned char* vs = sl + kScaleOff + 512 + kb * 64;
-        {
-            const uint32_t sel = (n & 1) ? 0x07060302u : 0x05040100u;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t t0 = *reinterpret_cast<const uint32_t*>(vs + 256 + 16 * k + (n & 2) * 2), t1 = *reinterpret_cast<const uint32_t*>(vs + 256 + 16 * k + 8 + (n & 2) * 2);
-                z.r[k] = __builtin_amdgcn_perm(t1, t0, sel);
-            }
-        }
-        zsum = __builtin_amdgcn_mfma_f32_16x16x32_f16(z.h, fb.h, zsum, 0, 0, 0);       // rows = channel groups
-        Frag sv[NS];
-        if constexpr (HP == 2) {
-            const uint32_t sel = (my_group & 1) ? 0x07060302u : 0x05040100u;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t t0 = *reinterpret_cast<const uint32_t*>(vs + 16 * k + (my_group & 2) * 2), t1 = *reinterpret_cast<const uint32_t*>(vs + 16 * k + 8 + (my_group & 2) * 2);
-                sv[0].r[k] = __builtin_amdgcn_perm(t1, t0, sel);
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint4v t = *reinterpret_cast<const uint4v*>(vs + 16 * k);         // tokens 2 k and 2 k + 1, four groups each
-                if constexpr (HP == 4) {
-                    const uint32_t sel = my_group ? 0x07060302u : 0x05040100u;
-                    sv[0].r[k] = __builtin_amdgcn_perm(t[2], t[0], sel);
-                    sv[1].r[k] = __builtin_amdgcn_perm(t[3], t[1], sel);
-                } else {
-                    sv[0].r[k] = __builtin_amdgcn_perm(t[2], t[0], 0x05040100u);
-                    sv[1].r[k] = __builtin_amdgcn_perm(t[2], t[0], 0x07060302u);
-                    sv[2].r[k] = __builtin_amdgcn_perm(t[3], t[1], 0x05040100u);
-                    sv[3].r[k] = __builtin_amdgcn_perm(t[3], t[1], 0x07060302u);
+                for (int k = 0; k < 4; ++k) {
+                    kw[4 * pl + k] = a[k];
+                    vw[4 * pl + k] = b[k];
                 }
             }
+            _Float16* operand = sm_operand[wave];
+            half2v hi, lo;
+            const bool big = any_above(k_scale, kKeyScaleLimit);
+            const float f = big ? 1.f / (1 << kKeyScaleShift) : 1.f;
+            split_products(__builtin_bit_cast(half2v, k_scale), own_q[0] * f, own_q[1] * f, own_q_up[0] * f, own_q_up[1] * f, hi, lo);
+            *reinterpret_cast<half2v*>(operand + 2 * lane) = hi;
+            *reinterpret_cast<half2v*>(operand + kKeyColumn + 2 * lane) = lo;
+            wave_lds_sync();
+            half8 kf[4];
+#pragma unroll
+            for (int cb = 0; cb < 4; ++cb) kf[cb] = *reinterpret_cast<const half8*>(operand + (is_lo ? kKeyColumn : 0) + cb * 32 + kb * 8);
+            const float zk = wave_sum(__builtin_amdgcn_fdot2(own_qz, __builtin_bit_cast(half2v, k_zero), 0.f, false)) * c_zero;
+            float4v d0 = {0.f, 0.f, 0.f, 0.f}, d1 = d0;
+#pragma unroll
+            for (int cb = 0; cb < 4; ++cb) {
+                d0 = __builtin_amdgcn_mfma_f32_16x16x32_f16(key_fragment<BITS>(kw, cb, 0), kf[cb], d0, 0, 0, 0);
+                d1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(key_fragment<BITS>(kw, cb, 1), kf[cb], d1, 0, 0, 0);
+            }
+            auto own_of = [&](const float4v& x) -> float {
+                const float a = own_i & 1 ? x[1] : x[0], b = own_i & 1 ? x[3] : x[2];
+                return own_i & 2 ? b : a;
+            };
+            // the token's sum over the rounded products from one column of the pair, over the remainders from the other
+            const float x0 = own_of(d0), x1 = own_of(d1), c = big ? c_code * (float)(1 << kKeyScaleShift) : c_code;
+            float x = fmaf(is_lo ? x1 : x0, is_lo ? c * kLoShrink : c, fmaf(dpp<kRor8>(is_lo ? x0 : x1), is_lo ? c : c * kLoShrink, zk));
+            if (r * kTileTokens < v.lowest) {
+                const int t = r * kTileTokens + own_tok;
+                x = ((t >= v.lowest) | (t < v.sinks)) ? x : -INFINITY;
+            }
+            if (__any(x > m + kSlack)) {
+                const float mn = fmaxf(m, wave_max(x)), g = __builtin_amdgcn_exp2f(m - mn);
+                rescale_acc(g);
+                l *= g;
+                m = mn;
+            }
+            if (prob_exp > 0.f && any_above(v_scale, kValueScaleLimit<BITS>)) {
+                const float g = __builtin_amdgcn_exp2f(-(float)kSlack - prob_exp);
+                rescale_acc(g);
+                l *= g;
+                prob_exp = -(float)kSlack;
+            }
+            const float pv = __builtin_amdgcn_exp2f(x + (prob_exp - own_exp - m)), pv_up = pv * kLoMagnify;
+            const half2v vz = __builtin_bit_cast(half2v, v_zero);
+            l_own += pv;
+            z_own[0] = fmaf(pv, (float)vz[0], z_own[0]);
+            z_own[1] = fmaf(pv, (float)vz[1], z_own[1]);
+            split_products(__builtin_bit_cast(half2v, v_scale), pv, pv, pv_up, pv_up, hi, lo);
+            wave_lds_sync();
+            _Float16* column = operand + own_pair * 4 * 32 + own_tok;       // columns (group, rounded / remainder)
+            column[0] = hi[0];
+            column[32] = lo[0];
+            column[64] = hi[1];
+            column[96] = lo[1];
+            wave_lds_sync();
+            const half8 vf = *reinterpret_cast<const half8*>(operand + (my_group * 2 + (is_lo ? 1 : 0)) * 32 + kb * 8);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value_fragment<BITS>(vw, u >> 1, u & 1), vf, acc[u], 0, 0, 0);
+            wave_lds_sync();
         }
+    };
+    auto record_many = [&](const unsigned char* sl, const View& v, int r) {
+        if constexpr (HP > 1) {
+            uint32_t w[2 * BITS];
 #pragma unroll
-        for (int pl = 0; pl < kPlanes; ++pl) {
-            const uint4v q4 = *reinterpret_cast<const uint4v*>(sl + kScaleOff + 1024 + pl * 1024 + lane16);
+            for (int pl = 0; pl < kPlanes; ++pl) {
+                const uint4v q4 = *reinterpret_cast<const uint4v*>(sl + pl * 1024 + (kb * 16 + row_pos) * 16);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) w[4 * pl + k] = q4[k];
-        }
-        if constexpr (BITS == 2) {
-            const half2v pf = {(_Float16)0.25f, (_Float16)0.25f};
-            fa.p[1] *= pf; fa.p[3] *= pf;
-            fb.p[1] *= pf; fb.p[3] *= pf;
-        }
-        Frag f[NS];
+                for (int k = 0; k < 4; ++k) w[4 * pl + k] = q4[k];
+            }
+            const bool big = any_above(*reinterpret_cast<const uint32_t*>(sl + kScaleOff + lane * 4), kKeyScaleLimit);
+            float4v d0 = {0.f, 0.f, 0.f, 0.f}, d1 = d0, dz = d0;
+            Frag s[4];
 #pragma unroll
-        for (int g = 0; g < NS; ++g)
+            for (int cb = 0; cb < 4; ++cb) {
+                s[cb].v = *reinterpret_cast<const uint4v*>(sl + kScaleOff + cb * 64 + kb * 16);
+                if constexpr (HP >= 8) {
+                    Frag z;
+                    z.v = *reinterpret_cast<const uint4v*>(sl + kScaleOff + 256 + cb * 64 + kb * 16);
+                    dz = __builtin_amdgcn_mfma_f32_16x16x32_f16(z.h, query_frag(cb), dz, 0, 0, 0);
+                }
+            }
+            if constexpr (HP < 8) {
+                // (eight channels in each of the four columns that share a head and kb)
+                Frag z;
+                z.v = *reinterpret_cast<const uint4v*>(sl + kScaleOff + 256 + (n >> 2) * 64 + kb * 16);
+                float sum = 0.f;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const half2v t = fa.p[k] * sv[g].p[k];
-                f[g].p[k] = __builtin_elementwise_fma(fb.p[k], sv[g].p[k], __builtin_elementwise_fma(fa.p[k], sv[g].p[k], -t));
+                for (int k = 0; k < 4; ++k) sum = __builtin_amdgcn_fdot2(q_zero[k], z.p[k], sum, false);
+                sum += dpp<kRor8>(sum);
+                sum += dpp<kRor4>(sum);
+                dz[0] = add_rows(sum);
+            }
+            if (big) {
+                const half2v f = {(_Float16)(1.f / (1 << kKeyScaleShift)), (_Float16)(1.f / (1 << kKeyScaleShift))};
+#pragma unroll
+                for (int cb = 0; cb < 4; ++cb)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) s[cb].p[k] *= f;
             }
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
-            acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value_fragment<BITS>(w, u >> 1, u & 1), f[(u >> 1) * NS / 4].h, acc[u], 0, 0, 0);
+            for (int cb = 0; cb < 4; ++cb) {
+                Frag f;
+                // in the lo columns alone; the hi columns' zeros stay
+                uint64_t active;
+                asm("s_and_saveexec_b64 %4, %13\n\tv_pk_mul_f16 %0, %5, %9\n\tv_pk_mul_f16 %1, %6, %10\n\tv_pk_mul_f16 %2, %7, %11\n\tv_pk_mul_f16 %3, %8, %12\n\ts_mov_b64 exec, %4"
+                    : "+&v"(rounded[0]), "+&v"(rounded[1]), "+&v"(rounded[2]), "+&v"(rounded[3]), "=&s"(active)
+                    : "v"(qk[cb][0]), "v"(qk[cb][1]), "v"(qk[cb][2]), "v"(qk[cb][3]), "v"(s[cb].p[0]), "v"(s[cb].p[1]), "v"(s[cb].p[2]), "v"(s[cb].p[3]), "s"(kLoColumns)
+                    : "scc");
+#pragma unroll
+                for (int k = 0; k < 4; ++k) f.p[k] = __builtin_elementwise_fma(qk[cb][k], s[cb].p[k], -rounded[k]);
+                d0 = __builtin_amdgcn_mfma_f32_16x16x32_f16(key_fragment<BITS>(w, cb, 0), f.h, d0, 0, 0, 0);
+                d1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(key_fragment<BITS>(w, cb, 1), f.h, d1, 0, 0, 0);
+            }
+            float x[4], pv[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                // hi and lo column of a head share its tokens: hi columns take tok0 + k, lo columns 16 + tok0 + k
+                x[k] = is_lo ? d1[k] : d0[k];
+                x[k] += dpp<kRor8>(is_lo ? d0[k] : d1[k]);
+            }
+            if (prob_exp > 0.f && any_above(*reinterpret_cast<const uint32_t*>(sl + kScaleOff + 512 + lane * 4), kValueScaleLimit<BITS>)) {
+                const float f = __builtin_amdgcn_exp2f(-(float)kSlack - prob_exp);
+                rescale_acc(f);
+                l *= f;
+                prob_exp = -(float)kSlack;
+            }
+            if (r * kTileTokens < v.lowest) mask(v, r * kTileTokens, x);
+            softmax(x, big ? c_code * (float)(1 << kKeyScaleShift) : c_code, dz[0] * c_zero, pv, rescale_acc);
+            // outputs: this lane's tokens 8 kb .. 8 kb + 7, as pairs, of a channel group
+            Frag fa, fb, z;
+            split(pv, fa, fb);
+            const unsigned char* vs = sl + kScaleOff + 512 + kb * 64;
+            {
+                const uint32_t sel = (n & 1) ? 0x07060302u : 0x05040100u;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t t0 = *reinterpret_cast<const uint32_t*>(vs + 256 + 16 * k + (n & 2) * 2), t1 = *reinterpret_cast<const uint32_t*>(vs + 256 + 16 * k + 8 + (n & 2) * 2);
+                    z.r[k] = __builtin_amdgcn_perm(t1, t0, sel);
+                }
+            }
+            zsum = __builtin_amdgcn_mfma_f32_16x16x32_f16(z.h, fb.h, zsum, 0, 0, 0);       // rows = channel groups
+            Frag sv[NS];
+            if constexpr (HP == 2) {
+                const uint32_t sel = (my_group & 1) ? 0x07060302u : 0x05040100u;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t t0 = *reinterpret_cast<const uint32_t*>(vs + 16 * k + (my_group & 2) * 2), t1 = *reinterpret_cast<const uint32_t*>(vs + 16 * k + 8 + (my_group & 2) * 2);
+                    sv[0].r[k] = __builtin_amdgcn_perm(t1, t0, sel);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint4v t = *reinterpret_cast<const uint4v*>(vs + 16 * k);         // tokens 2 k and 2 k + 1, four groups each
+                    if constexpr (HP == 4) {
+                        const uint32_t sel = my_group ? 0x07060302u : 0x05040100u;
+                        sv[0].r[k] = __builtin_amdgcn_perm(t[2], t[0], sel);
+                        sv[1].r[k] = __builtin_amdgcn_perm(t[3], t[1], sel);
+                    } else {
+                        sv[0].r[k] = __builtin_amdgcn_perm(t[2], t[0], 0x05040100u);
+                        sv[1].r[k] = __builtin_amdgcn_perm(t[2], t[0], 0x07060302u);
+                        sv[2].r[k] = __builtin_amdgcn_perm(t[3], t[1], 0x05040100u);
+                        sv[3].r[k] = __builtin_amdgcn_perm(t[3], t[1], 0x07060302u);
+                    }
+                }
+            }
+#pragma unroll
+            for (int pl = 0; pl < kPlanes; ++pl) {
+                const uint4v q4 = *reinterpret_cast<const uint4v*>(sl + kScaleOff + 1024 + pl * 1024 + lane16);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[4 * pl + k] = q4[k];
+            }
+            if constexpr (BITS == 2) {
+                const half2v pf = {(_Float16)0.25f, (_Float16)0.25f};
+                fa.p[1] *= pf; fa.p[3] *= pf;
+                fb.p[1] *= pf; fb.p[3] *= pf;
+            }
+            Frag f[NS];
+#pragma unroll
+            for (int g = 0; g < NS; ++g)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const half2v t = fa.p[k] * sv[g].p[k];
+                    f[g].p[k] = __builtin_elementwise_fma(fb.p[k], sv[g].p[k], __builtin_elementwise_fma(fa.p[k], sv[g].p[k], -t));
+                }
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value_fragment<BITS>(w, u >> 1, u & 1), f[(u >> 1) * NS / 4].h, acc[u], 0, 0, 0);
+        }
+    };
+    auto record_tile = [&](const unsigned char* sl, const View& v, int r) {
+        if constexpr (HP == 1) record_one(sl, v, r);
+        else record_many(sl, v, r);
     };
 
     // ---- 32 fp16 rows: keys are operands as they are; value rows, eight tokens by eight channels per lane, are turned in registers ----
@@ -676,7 +807,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
         }
     };
     // the lane of a head's pair of columns that holds channels 16 u + 4 kb .. of it
-    auto holds = [&](int u) { return !is_lo && (HP == 8 || (HP == 4 ? my_group == ((u >> 1) & 1) : my_group == (u >> 1))); };
+    auto holds = [&](int u) { return !is_lo && (HP == 1 ? n < 4 && my_group == (u >> 1) : HP == 8 || (HP == 4 ? my_group == ((u >> 1) & 1) : my_group == (u >> 1))); };
 
     bool first_unit = true;
     int slot = 0;
@@ -706,13 +837,15 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
                 raw[cb].v = *reinterpret_cast<const uint4v*>(p.q + (q_row + min(head, live - 1)) * kHeadDim + cb * 32 + kb * 8);
                 r8[cb] = raw[cb].h;
             }
-            set_query(r8);
+            half2v own = {(_Float16)0.f, (_Float16)0.f};
+            if constexpr (HP == 1) own = *reinterpret_cast<const half2v*>(p.q + q_row * kHeadDim + 2 * lane);
+            set_query(r8, own);
         }
 #pragma unroll
         for (int u = 0; u < 8; ++u) acc[u] = float4v{0.f, 0.f, 0.f, 0.f};
         zsum = float4v{0.f, 0.f, 0.f, 0.f};
         m = kNothing;
-        l = 0.f;
+        l = l_own = z_own[0] = z_own[1] = 0.f;
         prob_exp = (float)kProbExp<BITS>;
 #pragma unroll 1
         while (in_flight < NB) {
@@ -768,7 +901,8 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
         }
         // ---- leave the unit ----
         {
-            const float lw = add_rows(l + dpp<kRor8>(l));
+            float lw = add_rows(l + dpp<kRor8>(l));
+            if constexpr (HP == 1) lw += wave_sum(l_own * (BITS == 2 && (own_i & 2) ? 2.f : 0.5f));      // (every token is two lanes')
             if (lane < HP) {
                 sm_ml[wave][lane][0] = m - prob_exp;                   // sums and outputs are relative to 2^this
                 sm_ml[wave][lane][1] = lw;
@@ -787,16 +921,26 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
             }
         };
         const int c2 = (tid & 63) * 2, my_part = wg * 2 + (first_unit ? 0 : 1);
-        float zz[4];
+        float zz[4];                                                   // zero-points' share of this lane's head, by channel group
+        if constexpr (HP == 1) {
 #pragma unroll
-        for (int g = 0; g < 4; ++g) zz[g] = zsum[g] + dpp<kRor8>(zsum[g]);
+            for (int k = 0; k < 2; ++k) {
+                float t = z_own[k] * (BITS == 2 && (own_i & 2) ? 4.f : 1.f);
+                t += dpp<kXor2>(t);
+                t += dpp<kRor4>(t);
+                zz[k] = zz[k + 2] = add_rows(t + dpp<kRor8>(t));
+            }
+        } else {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) zz[g] = zsum[g] + dpp<kRor8>(zsum[g]);
+        }
 #pragma unroll 1
         for (int g0 = 0; g0 < HP; g0 += HR) {
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
                 float4v o;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = fmaf(acc[u][i] + dpp<kRor8>(acc[u][i]), kValueUnscale, zz[u >> 1]);
+                for (int i = 0; i < 4; ++i) o[i] = fmaf(HP == 1 ? fmaf(dpp<kRor8>(acc[u][i]), kLoShrink, acc[u][i]) : acc[u][i] + dpp<kRor8>(acc[u][i]), kValueUnscale, zz[u >> 1]);
                 if (holds(u) && head >= g0 && head < g0 + HR) *reinterpret_cast<float4v*>(&sm_o[wave][head - g0][u * 16 + kb * 4]) = o;
             }
             lds_barrier();
@@ -892,11 +1036,13 @@ hipError_t launch_paged_attention(const PagedAttentionParams& params, hipStream_
     p.part_ml = p.part_o + (size_t)kWorkgroups * 2 * kMaxHeads * kPartFloats;
 #define KIVI_PAGED(B, H) paged_attention_kernel<B, H><<<kWorkgroups, 64 * kWaves, 0, stream>>>(p)
     if (p.bits == 2) {
-        if (p.run <= 2) KIVI_PAGED(2, 2);
+        if (p.run == 1) KIVI_PAGED(2, 1);
+        else if (p.run == 2) KIVI_PAGED(2, 2);
         else if (p.run <= 4) KIVI_PAGED(2, 4);
         else KIVI_PAGED(2, 8);
     } else {
-        if (p.run <= 2) KIVI_PAGED(4, 2);
+        if (p.run == 1) KIVI_PAGED(4, 1);
+        else if (p.run == 2) KIVI_PAGED(4, 2);
         else if (p.run <= 4) KIVI_PAGED(4, 4);
         else KIVI_PAGED(4, 8);
     }

@@ -141,7 +141,7 @@ LENGTHS = [1, 2, 31, 32, 33, 63, 64, 65, 95, 96, 97, 127, 128, 129, 160, 191, 22
 
 
 @pytest.mark.parametrize("bits,q_heads,kv_heads,page,residual", [
-    (2, 4, 4, 64, 64), (4, 4, 2, 32, 64), (2, 12, 3, 128, 96), (4, 8, 1, 64, 32), (2, 16, 2, 32, 128), (4, 11, 1, 256, 64), (2, 3, 1, 64, 0),
+    (2, 4, 4, 64, 64), (4, 3, 3, 128, 64), (4, 4, 2, 32, 64), (2, 12, 3, 128, 96), (4, 8, 1, 64, 32), (2, 16, 2, 32, 128), (4, 11, 1, 256, 64), (2, 3, 1, 64, 0),
 ])
 def test_prompts_of_all_lengths(bits, q_heads, kv_heads, page, residual):
     print(f"case paged prompts bits={bits} heads={q_heads}/{kv_heads} page={page} R={residual}", flush=True)
@@ -187,9 +187,10 @@ def test_wide_groups(bits, q_heads, kv_heads):
     run.attention(window=120, sinks=3)
 
 
+@pytest.mark.parametrize("q_heads", [2, 6])
 @pytest.mark.parametrize("scale", [0.0, -0.05])
-def test_softmax_scales(scale):
-    run = Run(2, 6, 2, 2)
+def test_softmax_scales(scale, q_heads):
+    run = Run(2, q_heads, 2, 2)
     run.append([400, 70])
     run.attention(scale=scale)
     run.attention(scale=scale, window=100, sinks=33)
@@ -277,11 +278,12 @@ def test_two_rows_of_one_sequence_and_prefix_pages():
     assert (out[1] - alone[0]).abs().max() <= 2 * 2.0 ** -11 * alone.abs().max()
 
 
+@pytest.mark.parametrize("q_heads,kv_heads", [(4, 2), (2, 2), (7, 1)])
 @pytest.mark.parametrize("bits,scale", [(2, 40.0), (4, 40.0), (2, 3000.0), (4, 3000.0), (2, 1e-3)])
-def test_scales_out_of_the_ordinary(bits, scale):
+def test_scales_out_of_the_ordinary(bits, scale, q_heads, kv_heads):
     """Keys and values whose group scales pass what the operands hold without a shift, next to small ones."""
-    print(f"case paged scales bits={bits} values times {scale}", flush=True)
-    run = Run(2, 4, 2, bits, most=400)
+    print(f"case paged scales bits={bits} heads={q_heads}/{kv_heads} values times {scale}", flush=True)
+    run = Run(2, q_heads, kv_heads, bits, most=400)
     plain = run.new_rows
 
     def rows(n):
@@ -303,6 +305,11 @@ def test_long_sequences_are_divided():
     run.attention()
     run.attention(window=4000, sinks=70)
     run.attention()                                    # (the workspace is ready for the next call)
+    for bits in (2, 4):
+        one = Run(2, 1, 1, bits, most=9000, page=512, residual=128)
+        one.append([8999, 5000])
+        one.attention()
+        one.attention(window=700, sinks=300)
     many = Run(150, 6, 3, 4, most=192)
     many.append([int(x) for x in np.random.default_rng(3).integers(1, 190, 150)])
     many.check_cache()
