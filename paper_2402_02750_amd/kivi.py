@@ -210,11 +210,14 @@ def kivi_decode_workspace_bytes(layout: kivi_layout_t) -> int:
     return n.value
 
 
-def _stream_handle(stream) -> Optional[int]:
+def _stream_handle(stream, device=None) -> Optional[int]:
     if stream is None:
         import torch
-        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))     # (current_stream() takes 2.8 us)
-    return ctypes.c_void_p(stream.cuda_stream)
+        # (current_stream() takes 2.8 us)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device is None else device)
+    if device is not None and stream.device_index != device:
+        raise KiviError(KIVI_ERR_INVALID_ARG, f"stream of cuda:{stream.device_index}, the current device is cuda:{device}")
+    return stream.cuda_stream
 
 
 def _strides_bht(x):
@@ -421,30 +424,34 @@ _QUERY = struct.Struct("PPiiif")
 _ROTATION = struct.Struct("PPiii4x")
 
 
+_kinds = {}                          # KIVI_TYPE_* by torch type
+
+
 def _type_of(x) -> int:
-    import torch
-    dtype = x.dtype
-    if dtype is torch.float16:
-        return KIVI_TYPE_FP16
-    if dtype is torch.bfloat16:
-        return KIVI_TYPE_BF16
-    raise KiviError(KIVI_ERR_UNSUPPORTED, f"tensor of {dtype}")
+    kind = _kinds.get(x.dtype)
+    if kind is None:
+        import torch
+        _kinds.update({torch.float16: KIVI_TYPE_FP16, torch.bfloat16: KIVI_TYPE_BF16})
+        if x.dtype not in _kinds:
+            raise KiviError(KIVI_ERR_UNSUPPORTED, f"tensor of {x.dtype}")
+        return _kinds[x.dtype]
+    return kind
 
 
-def _on_device(*tensors):
-    """All tensors on the current device: its stream and launches are the ones the library uses."""
+def _on_device(*tensors) -> int:
+    """All tensors on the current device, which is returned: its stream and launches are the ones the library uses."""
     import torch
     here = torch.cuda.current_device()
     for x in tensors:
         if x is not None and x.get_device() != here:
             raise KiviError(KIVI_ERR_INVALID_ARG, f"tensor on {x.device}, the current device is cuda:{here}")
+    return here
 
 
-def _rows(x, rows, heads=0):
-    """[rows, heads, 128] (any row and head strides) as the fields of a kivi_tensor_t."""
-    n, h, d = x.shape
+def _rows(x, shape):
+    """A tensor of this shape, [rows, heads, 128] (any row and head strides), as the fields of a kivi_tensor_t."""
     st, sh, sd = x.stride()
-    assert n == rows and (h == heads or not heads) and d == 128 and sd == 1, f"expected [{rows}, {heads or 'heads'}, 128] with contiguous channels"
+    assert x.shape == shape and sd == 1, f"expected {list(shape)} with contiguous channels"
     return x.data_ptr(), 0, sh, st
 
 
@@ -486,27 +493,30 @@ def kivi_norm_rotate(q, q_out, k=None, k_out=None, q_weight=None, k_weight=None,
                      rotation: Optional[Rotation] = None, positions=None, stream=None):
     """q, k: CUDA fp16 / bf16 [rows, heads, 128] (any row and head strides); q_out, k_out the same shapes, fp16 or bf16, maybe q
     and k themselves; weights: [128] in the type of q / k, or None (no norm); positions: int32 [rows]."""
-    _on_device(q, q_out, k, k_out, q_weight, k_weight, positions, rotation.table if rotation else None)
+    here = _on_device(q, q_out, k, k_out, q_weight, k_weight, positions, rotation.table if rotation else None)
     rows, heads, _ = q.shape
-    job = (*_rows(q, rows), *_rows(q_out, rows, heads), _weight(q_weight, q), weight_offset, heads, _type_of(q), _type_of(q_out))
+    shape = rows, heads, 128
+    job = (*_rows(q, shape), *_rows(q_out, shape), _weight(q_weight, q), weight_offset, heads, _type_of(q), _type_of(q_out))
     if k is None:
         n, jobs = 1, _JOB.pack(*job)
     else:
         heads = k.shape[1]
-        n, jobs = 2, _TWO_JOBS.pack(*job, *_rows(k, rows), *_rows(k_out, rows, heads), _weight(k_weight, k), weight_offset, heads,
+        shape = rows, heads, 128
+        n, jobs = 2, _TWO_JOBS.pack(*job, *_rows(k, shape), *_rows(k_out, shape), _weight(k_weight, k), weight_offset, heads,
                                     _type_of(k), _type_of(k_out))
     r = None
     if rotation is not None:
         assert positions is not None, "a rotation needs positions"
-        r = _ROTATION.pack(rotation._fields[0], _int32(positions, rows) or 0, *rotation._fields[1:])
-    _check(load_library().kivi_norm_rotate(jobs, n, rows, eps, r, _stream_handle(stream)), "kivi_norm_rotate")
+        table, *rest = rotation._fields
+        r = _ROTATION.pack(table, _int32(positions, rows) or 0, *rest)
+    _check(load_library().kivi_norm_rotate(jobs, n, rows, eps, r, _stream_handle(stream, here)), "kivi_norm_rotate")
 
 
 def kivi_prompt_attention(q, k, v, out, softmax_scale, q_starts=None, k_starts=None, max_q=None, max_k=None, window=0, sinks=0, stream=None):
     """Either q, out [b, H_q, n_q, 128] and k, v [b, H_kv, n_k, 128] (any strides), or, with q_starts and k_starts (int32
     [b + 1]), rows of sequences one after the other: q, out [rows, H_q, 128], k, v [rows, H_kv, 128] and max_q, max_k the longest
     sequence's.  fp16 or bf16, all alike."""
-    _on_device(q, k, v, out, q_starts, k_starts)
+    here = _on_device(q, k, v, out, q_starts, k_starts)
     kind = _type_of(q)
     assert _type_of(k) == _type_of(v) == _type_of(out) == kind, "q, k, v and out have one type"
     if q_starts is not None:
@@ -516,7 +526,8 @@ def kivi_prompt_attention(q, k, v, out, softmax_scale, q_starts=None, k_starts=N
         k_rows, kv_heads, _ = k.shape
         p = _PROMPT.pack(batch, heads, kv_heads, 128, kind, max_q, max_k, _int32(q_starts), _int32(k_starts, batch + 1), q_rows, k_rows, window, sinks,
                          softmax_scale)
-        tensors = _rows(q, q_rows), _rows(k, k_rows), _rows(v, k_rows, kv_heads), _rows(out, q_rows, heads)
+        q_shape, k_shape = (q_rows, heads, 128), (k_rows, kv_heads, 128)
+        tensors = _rows(q, q_shape), _rows(k, k_shape), _rows(v, k_shape), _rows(out, q_shape)
     else:
         assert k_starts is None and out.shape == q.shape and v.shape == k.shape, "out is shaped like q, v like k"
         batch, heads, max_q, d = q.shape
@@ -532,7 +543,7 @@ def kivi_prompt_attention(q, k, v, out, softmax_scale, q_starts=None, k_starts=N
         with torch.cuda.stream(stream):                 # (the allocator orders its reuse by this stream)
             workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
     _check(lib.kivi_prompt_attention(p, *[_ONE_TENSOR.pack(*t) for t in tensors], workspace.data_ptr() if need.value else None, need.value,
-                                     _stream_handle(stream)), "kivi_prompt_attention")
+                                     _stream_handle(stream, here)), "kivi_prompt_attention")
     return out
 
 
@@ -606,30 +617,31 @@ def kivi_paged_append(cache: PagedCache, batch: PagedBatch, k, v, starts=None, m
     """k, v: CUDA fp16 / bf16 [rows, H_kv, 128] (any row and head strides), the new rows of all sequences: those of
     sequence b are rows starts[b] .. starts[b + 1] - 1 (int32 [b + 1]), or max_new of each without starts.  batch.lengths counts them
     already.  q [rows, H_q, 128] is rotated into q_out (fp16)."""
-    _on_device(k, v, starts, positions, q, q_out, batch.lengths, cache.workspace, rotation.table if rotation else None)
+    here = _on_device(k, v, starts, positions, q, q_out, batch.lengths, cache.workspace, rotation.table if rotation else None)
     l, n = cache.layout, k.shape[0]
-    heads = l.n_kv_heads
+    shape = n, l.n_kv_heads, 128
     assert v.dtype is k.dtype, "k, v and q have one type"
     qs = _NO_TENSOR * 2
     if q is not None:
         assert q.dtype is k.dtype and _type_of(q_out) == KIVI_TYPE_FP16, "q has the type of k, q_out is fp16"
-        qs = (*_rows(q, n, l.n_q_heads), *_rows(q_out, n, l.n_q_heads))
+        q_shape = n, l.n_q_heads, 128
+        qs = (*_rows(q, q_shape), *_rows(q_out, q_shape))
     else:
         assert q_out is None, "q_out without q"
     r, at = None, 0
     if rotation is not None:
         r = rotation.c(positions, n)
         at = ctypes.addressof(r)
-    rows = _ROWS.pack(*_rows(k, n, heads), *_rows(v, n, heads), *qs, _type_of(k), n, max_new, _int32(starts, batch.size + 1) or 0, at)
-    _check(load_library().kivi_paged_append(*cache._refs, batch._ref, rows, _stream_handle(stream)), "kivi_paged_append")
+    rows = _ROWS.pack(*_rows(k, shape), *_rows(v, shape), *qs, _type_of(k), n, max_new, _int32(starts, batch.size + 1) or 0, at)
+    _check(load_library().kivi_paged_append(*cache._refs, batch._ref, rows, _stream_handle(stream, here)), "kivi_paged_append")
 
 
 def kivi_paged_attention(cache: PagedCache, batch: PagedBatch, q_fp16, softmax_scale, out, window=0, sinks=0, stream=None):
     """q_fp16: contiguous CUDA fp16 [b, H_q, 128]; out: the same shape, contiguous, fp16 or bf16."""
-    _on_device(q_fp16, out, batch.lengths, cache.workspace)
+    here = _on_device(q_fp16, out, batch.lengths, cache.workspace)
     assert _type_of(q_fp16) == KIVI_TYPE_FP16 and q_fp16.is_contiguous() and out.is_contiguous(), "q is fp16; q and out are contiguous"
     shape = q_fp16.shape
     assert shape == out.shape and shape == (batch.size, cache.layout.n_q_heads, 128), "q and out are [b, H_q, 128]"
     query = _QUERY.pack(q_fp16.data_ptr(), out.data_ptr(), _type_of(out), window, sinks, softmax_scale)
-    _check(load_library().kivi_paged_attention(*cache._refs, batch._ref, query, *cache._workspace, _stream_handle(stream)), "kivi_paged_attention")
+    _check(load_library().kivi_paged_attention(*cache._refs, batch._ref, query, *cache._workspace, _stream_handle(stream, here)), "kivi_paged_attention")
     return out

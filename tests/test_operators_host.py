@@ -241,3 +241,12 @@ def test_page_tables_whose_rows_overlap_are_refused(lib):
     b = kivi.PagedBatch(torch.zeros(3, 8, dtype=torch.int32)[:, :4], lengths)
     assert (b.c.batch, b.c.max_pages, b.c.page_table_stride) == (3, 4, 8)
     assert kivi.PagedBatch(torch.zeros(1, 4, dtype=torch.int32).expand(1, 4), lengths[:1]).c.page_table_stride >= 4
+
+
+def test_stream_of_another_device():
+    class Stream:
+        device_index, cuda_stream = 1, 0x1000
+    assert kivi._stream_handle(Stream(), 1) == 0x1000
+    with pytest.raises(kivi.KiviError) as e:
+        kivi._stream_handle(Stream(), 0)
+    assert e.value.status == INVALID
