@@ -50,9 +50,10 @@ union Frag {                           // one lane's share of an operand: eight 
 
 constexpr int kWaves = 4;
 constexpr int kWorkgroups = 768;       // three per compute unit; a multiple of the eight dies
-// Costs in steps of records.  Of a step of fp16 rows (1, 2, 3, 4: 16 x 32 767 tokens, 64 / 8 heads, 4 bits 125.7, 126.8, 130.3, 126.3 us; 32 x 16 001 tokens,
-// window 4096 108, 101, 105, 107; 200 x 500-2000 tokens 75, 72, 74), and what a further unit in an interval costs (leaving one, entering the next).
-constexpr int kRowCost = 2, kEnterCost = 5;
+// What entering and leaving a unit costs in steps of records, before its first step on the axis.  (A step of fp16 rows is as many as one of records.
+// 0, 2, 3, 4 with rows 1; 0, 2, 3 with rows 2: 64 x 500-8000 tokens, 32 / 8 heads -, 60, 58.6, 61; 66, 61, 63 us; 200 x 500-2000 -, 63, 61, 64; 67, 66, 64;
+// 64 x 500-8000, 64 / 8 -, 71, 66, 67; 73, 70, 71.)
+constexpr int kUnitCost = 3;
 // Steps of an interval, at least (1, 2, 4, 8: one sequence of 3001 tokens 15.3, 15.3, 18.2, 25 us; 4 heads x 1023 tokens 11.0, 9.9, 11.7, 17; 8000 tokens, 32 / 8 heads 21.9, 18.0, 20.7, 26)
 constexpr int kMinCost = 2;
 constexpr int kScanned = 4;            // times 64 sequences whose costs stay in registers
@@ -201,7 +202,7 @@ struct View {
     int records, sink_records, skip;   // visible records: i < sink_records: i, else i + skip
     int row0, row_tiles;               // first token of the first tile of fp16 rows, tiles of 32
     int row_steps, steps;
-    __device__ __forceinline__ int cost() const { return row_steps * kRowCost + steps; }
+    __device__ __forceinline__ int cost() const { return row_steps + steps; }
 };
 __device__ __forceinline__ View view_of(const Args& p, int length) {
     View v;
@@ -265,13 +266,17 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
         if (i * 64 < p.batch) {
             if (i * 64 + lane < p.batch) tokens[i] = length_of(i * 64 + lane);
             costs[i] = cost_of(tokens[i]);
-            total += sum_all(costs[i]) * units_per_sequence;
-            units += __popcll(__ballot(costs[i] > 0)) * units_per_sequence;
+            const int some = __popcll(__ballot(costs[i] > 0));
+            total += (sum_all(costs[i]) + some * kUnitCost) * units_per_sequence;
+            units += some * units_per_sequence;
         }
     }
-    for (int b0 = kScanned * 64; b0 < p.batch; b0 += 64) total += sum_all(b0 + lane < p.batch ? cost_of(length_of(b0 + lane)) : 0) * units_per_sequence;
+    for (int b0 = kScanned * 64; b0 < p.batch; b0 += 64) {
+        const int cost = b0 + lane < p.batch ? cost_of(length_of(b0 + lane)) : 0;
+        total += sum_all(cost > 0 ? cost + kUnitCost : 0) * units_per_sequence;
+    }
     if (total == 0) return;
-    // An interval of `length` of the axis for every workgroup, or, where that costs little more, every unit cut evenly on its own: `length`
+    // An interval of `length` of the axis for every workgroup, or, where no piece gets longer, every unit cut evenly on its own: `length`
     // is then the longest piece, and no workgroup enters two units.
     int length = max((total + kWorkgroups - 1) / kWorkgroups, kMinCost);
     bool own_pieces = false;
@@ -283,9 +288,9 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
                 if (i * 64 < p.batch) n += sum_all((costs[i] + piece - 1) / piece) * units_per_sequence;
             return n <= kWorkgroups;
         };
-        own_pieces = fits(length + kEnterCost);
+        own_pieces = fits(length);
         if (own_pieces) {
-            int low = length, high = length + kEnterCost;
+            int low = max((total - units * kUnitCost + kWorkgroups - 1) / kWorkgroups, kMinCost), high = length;
             while (low < high) {
                 const int mid = (low + high) / 2;
                 if (fits(mid)) high = mid;
@@ -295,7 +300,8 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
         }
     }
     // what of the axis is in front of a sequence: workgroups with pieces of their own, cost otherwise
-    auto share_of = [&](int cost) { return (own_pieces ? (cost + length - 1) / length : cost) * units_per_sequence; };
+    const int unit_cost = own_pieces ? 0 : kUnitCost;
+    auto share_of = [&](int cost) { return (own_pieces ? (cost + length - 1) / length : cost > 0 ? cost + unit_cost : 0) * units_per_sequence; };
     const int x_first = own_pieces ? wg : wg * length;
     int b = -1, before = 0, n_tokens = 0;                              // the sequence of this workgroup's first unit, and where it begins
     {
@@ -323,11 +329,11 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
     before = __builtin_amdgcn_readfirstlane(before);
     n_tokens = __builtin_amdgcn_readfirstlane(n_tokens);
     if (b < 0) return;                                                 // (more workgroups than pieces, or than intervals)
-    // A place on the axis: sequence, unit in it, and where the unit begins
+    // A place on the axis: sequence, unit in it, and where the unit's steps begin
     struct Place { int b, unit, unit0; View view; };
     int x0, x1, pieces = 1, piece = 0;                                 // the interval; own pieces: of the unit
     auto next_unit = [&](Place& u) {                                   // (only where another one follows)
-        u.unit0 += u.view.cost();
+        u.unit0 += u.view.cost() + unit_cost;
         if (++u.unit == units_per_sequence) {
             u.unit = 0;
             int n = 0, slot = -1;
@@ -357,15 +363,16 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
             x0 = cost * piece / pieces;
             x1 = cost * (piece + 1) / pieces;
         } else {
-            here.unit = (x_first - before) / cost;
-            here.unit0 = before + here.unit * cost;
+            here.unit = (x_first - before) / (cost + unit_cost);
+            here.unit0 = before + here.unit * (cost + unit_cost) + unit_cost;
             x0 = x_first;
             x1 = min(x0 + length, total);
+            if (here.unit0 >= x1) return;                              // (nothing but what comes before the steps)
         }
     }
     // its steps of records in this interval: [first, end)
-    auto records_from = [&](const Place& u) { return max(x0 - u.unit0 - u.view.row_steps * kRowCost, 0); };
-    auto records_to = [&](const Place& u) { return u.view.records > 0 ? max(min(x1 - u.unit0, u.view.cost()) - u.view.row_steps * kRowCost, 0) : 0; };
+    auto records_from = [&](const Place& u) { return max(x0 - u.unit0 - u.view.row_steps, 0); };
+    auto records_to = [&](const Place& u) { return u.view.records > 0 ? max(min(x1 - u.unit0, u.view.cost()) - u.view.row_steps, 0) : 0; };
 
     // ---- copies of records into this wavefront's ring, NB ahead ----
     const uint32_t ring_lds = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)&sm_ring[wave][0][0]);
@@ -388,7 +395,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
     uint32_t lost = 0;                                                 // slots whose record has no page
     auto advance_copy = [&]() {
         while (c_left <= 0) {
-            if (cursor.unit0 + cursor.view.cost() >= x1) return;
+            if (cursor.unit0 + cursor.view.cost() + unit_cost >= x1) return;
             next_unit(cursor);
             enter_unit(0);
         }
@@ -853,17 +860,16 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
             advance_copy();
             if (in_flight == was) break;
         }
-        // steps of fp16 rows that begin in the interval
-        const int rows_cost = view.row_steps * kRowCost, row_end = min(x1 - here.unit0, rows_cost);
-        const int row_from = (min(max(x0 - here.unit0, 0), rows_cost) + kRowCost - 1) / kRowCost;
-        if (row_from * kRowCost < row_end) {
+        // its steps of fp16 rows in the interval
+        const int row_from = min(max(x0 - here.unit0, 0), view.row_steps), row_end = min(x1 - here.unit0, view.row_steps);
+        if (row_from < row_end) {
             const int slot_of_rows = p.slots ? scalar(p.slots, here.b) : here.b;
             const int64_t ring = ((int64_t)slot_of_rows * p.n_kv_heads + kvh) * p.cap_r * kHeadDim;
             float4v ro[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) ro[e] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-            for (int j = row_from; j * kRowCost < row_end; ++j)
+            for (int j = row_from; j < row_end; ++j)
                 if (j * kWaves + wave < view.row_tiles) row_tile(view, ring, j * kWaves + wave, ro);
             // into the records' order
 #pragma unroll
@@ -892,7 +898,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
         }
         const int j1 = records_to(here);
         for (int j = records_from(here); j < j1; ++j) {
-            progress(here.unit0 + rows_cost + j);
+            progress(here.unit0 + view.row_steps + j);
             wait_oldest();
             const int i = j * kWaves + wave;
             if (i < view.records && !((lost >> slot) & 1)) record_tile(&sm_ring[wave][slot][0], view, i < view.sink_records ? i : i + view.skip);
@@ -972,7 +978,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
             lds_barrier();
             if (sm_last) {
                 // the unit is the first one of every workgroup but, maybe, the first of them
-                const int second = !own_pieces && owner0 * length < here.unit0 ? 1 : 0;
+                const int second = !own_pieces && owner0 * length < here.unit0 - unit_cost ? 1 : 0;
                 constexpr int kBatch = 8;
                 for (int hh = wave; hh < live; hh += kWaves) {
                     float mm = kNothing, sum = 0.f, ox = 0.f, oy = 0.f;
@@ -1007,7 +1013,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
             }
             lds_barrier();
         }
-        if (here.unit0 + cost >= x1) break;
+        if (here.unit0 + cost + unit_cost >= x1) break;
         first_unit = false;
         next_unit(here);
     }
@@ -1029,7 +1035,7 @@ hipError_t launch_paged_attention(const PagedAttentionParams& params, hipStream_
     p.by_runs = FastDiv::by(p.runs);
     // (the axis has to fit 31 bits)
     const int64_t records = (int64_t)p.max_pages << p.page_shift, rows = (p.residual + 2 * kTileTokens) / kTileTokens;
-    const int64_t cost = (records + kWaves - 1) / kWaves + ((rows + kWaves - 1) / kWaves) * kRowCost;
+    const int64_t cost = (records + kWaves - 1) / kWaves + (rows + kWaves - 1) / kWaves + kUnitCost;
     if (cost > 0x200000 || cost * p.batch * p.n_kv_heads * p.runs > 0x40000000) return hipErrorNotSupported;
     char* ws = reinterpret_cast<char*>(p.counters);
     p.part_o = reinterpret_cast<float*>(ws + kWorkgroups * sizeof(int32_t));

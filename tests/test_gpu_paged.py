@@ -316,6 +316,20 @@ def test_long_sequences_are_divided():
     many.attention()
 
 
+@pytest.mark.parametrize("q_heads,kv_heads", [(1, 1), (8, 4)])
+@pytest.mark.parametrize("batch", [65, 257, 300])
+def test_batches_of_many_short_sequences(batch, q_heads, kv_heads):
+    """More sequences than a workgroup looks at in one go, short ones with a few long ones between, whole and through a window."""
+    print(f"case paged many batch={batch} heads={q_heads}/{kv_heads}", flush=True)
+    run = Run(batch, q_heads, kv_heads, 2, most=704, page=64)
+    lengths = np.random.default_rng(batch).integers(1, 41, batch)
+    lengths[::19] = 700
+    lengths[-1] = 333
+    run.append([int(x) for x in lengths])
+    run.attention()
+    run.attention(window=50, sinks=3)
+
+
 def test_graph_replays_follow_the_lengths():
     """A captured step (append with rotation, attention) replayed while lengths and pages move on, with eager calls between."""
     torch = gh.require_gpu()
