@@ -4,10 +4,11 @@
 // fp16 rows -- follows from the sequence's length, and is put on one axis for all units, in steps of one record or tile per
 // wavefront.  Every workgroup adds up the lengths by itself (sums across lanes without LDS) and takes one interval of the axis, so the
 // device is divided evenly whatever the lengths, and nothing but the batch's size is known to the host: a captured call follows lengths and
-// pages.  Where that leaves the longest piece little longer (few units, short ones), each unit is cut evenly on its own instead, and no workgroup
+// pages.  Where no piece gets longer (few units, short ones), each unit is cut evenly on its own instead, and no workgroup
 // enters two: 8 sequences of 500 tokens, 32 / 8 heads 20.6 -> 13.2 us.  A unit that lies in one interval is written out by it; of one that several
 // share each leaves a part (maximum, sum, outputs) in the workspace, and the last to come joins them.  A workgroup shares its first and its
-// last unit at most, so the workspace has two parts per workgroup whatever the batch; a unit is counted where its first workgroup is.
+// last unit at most, so the workspace has two parts per workgroup whatever the batch; a unit is counted where its first workgroup is.  Entering and leaving
+// a unit has its place on the axis too, in front of the unit's steps; an interval that begins in it begins with the steps.
 //
 // Products: 16x16x32 matrix instructions; operand rows are tokens (keys) and channels (values), columns are query heads.  Lane
 // (n = lane % 16, kb = lane / 16) makes the eight contraction elements 8 kb .. 8 kb + 7 of column n: head n % HP; n < 8: rounded products, n >= 8: what
@@ -25,10 +26,11 @@
 // registers: keys are operands as they are, value rows are turned by byte permutes.
 //
 // Bound: issue of vector instructions and memory, which overlap in part: of 64 sequences of 500-8000 tokens (32 / 8 heads, 2 bits, 257 MB) the copies
-// alone take 49 us, the arithmetic alone 46, both 62.5 (4.1 TB/s); 12 us of each are what a launch pays once (lengths, first page, first record: 5; leaving units,
+// alone take 49 us, the arithmetic alone 46, both 59 (4.4 TB/s); 12 us of each are what a launch pays once (lengths, first page, first record: 5; leaving units,
 // counting, joining: 7).  16 x 32 767 tokens, 64 / 8 heads, 4 bits 121 us (5.6 TB/s); 32 x 16 001 tokens, 32 heads, window 4096 82 (5.6 TB/s);
-// one sequence of 3001 tokens, 32 heads 14.3.  Four wavefronts per SIMD (128 registers) spill: 64 -> 104 us; a ring of four records at 2 bits, units counted
-// at the end of an interval, the first fp16 rows asked for with the query (spills): no gain.
+// one sequence of 3001 tokens, 32 heads 13.5.  Four wavefronts per SIMD (128 registers) spill: 64 -> 104 us; a ring of four records at 2 bits, units counted
+// at the end of an interval, the first fp16 rows asked for with the query (spills), priorities that also fall with a workgroup's age: no gain.  Operands
+// through LDS as at record_one for two and four heads as well: a sixth fewer vector instructions, as fast at 2 bits, 75 -> 83 us at 4.
 #include "kivi_paged.h"
 
 #include <algorithm>
@@ -54,7 +56,8 @@ constexpr int kWorkgroups = 768;       // three per compute unit; a multiple of 
 // 0, 2, 3, 4 with rows 1; 0, 2, 3 with rows 2: 64 x 500-8000 tokens, 32 / 8 heads -, 60, 58.6, 61; 66, 61, 63 us; 200 x 500-2000 -, 63, 61, 64; 67, 66, 64;
 // 64 x 500-8000, 64 / 8 -, 71, 66, 67; 73, 70, 71.)
 constexpr int kUnitCost = 3;
-// Steps of an interval, at least (1, 2, 4, 8: one sequence of 3001 tokens 15.3, 15.3, 18.2, 25 us; 4 heads x 1023 tokens 11.0, 9.9, 11.7, 17; 8000 tokens, 32 / 8 heads 21.9, 18.0, 20.7, 26)
+// Steps of an interval, at least (1, 2, 4, 8: one sequence of 3001 tokens 15.3, 15.3, 18.2, 25 us; 4 heads x 1023 tokens 11.0, 9.9, 11.7, 17; 8000 tokens,
+// 32 / 8 heads 21.9, 18.0, 20.7, 26)
 constexpr int kMinCost = 2;
 constexpr int kScanned = 4;            // times 64 sequences whose costs stay in registers
 constexpr int kMaxHeads = 8;           // query heads of a unit
@@ -568,7 +571,8 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
         if constexpr (HP == 1) {
             const unsigned char* scales = sl + kScaleOff;
             const uint32_t k_scale = *reinterpret_cast<const uint32_t*>(scales + lane * 4), k_zero = *reinterpret_cast<const uint32_t*>(scales + 256 + lane * 4);
-            const uint32_t v_scale = *reinterpret_cast<const uint32_t*>(scales + 512 + own_tok * 8 + own_pair * 4), v_zero = *reinterpret_cast<const uint32_t*>(scales + 768 + own_tok * 8 + own_pair * 4);
+            const unsigned char* own = scales + 512 + own_tok * 8 + own_pair * 4;
+            const uint32_t v_scale = *reinterpret_cast<const uint32_t*>(own), v_zero = *reinterpret_cast<const uint32_t*>(own + 256);
             uint32_t kw[2 * BITS], vw[2 * BITS];
 #pragma unroll
             for (int pl = 0; pl < kPlanes; ++pl) {
@@ -715,7 +719,8 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
                 const uint32_t sel = (n & 1) ? 0x07060302u : 0x05040100u;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const uint32_t t0 = *reinterpret_cast<const uint32_t*>(vs + 256 + 16 * k + (n & 2) * 2), t1 = *reinterpret_cast<const uint32_t*>(vs + 256 + 16 * k + 8 + (n & 2) * 2);
+                    const unsigned char* t = vs + 256 + 16 * k + (n & 2) * 2;
+                    const uint32_t t0 = *reinterpret_cast<const uint32_t*>(t), t1 = *reinterpret_cast<const uint32_t*>(t + 8);
                     z.r[k] = __builtin_amdgcn_perm(t1, t0, sel);
                 }
             }
@@ -725,7 +730,8 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
                 const uint32_t sel = (my_group & 1) ? 0x07060302u : 0x05040100u;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const uint32_t t0 = *reinterpret_cast<const uint32_t*>(vs + 16 * k + (my_group & 2) * 2), t1 = *reinterpret_cast<const uint32_t*>(vs + 16 * k + 8 + (my_group & 2) * 2);
+                    const unsigned char* t = vs + 16 * k + (my_group & 2) * 2;
+                    const uint32_t t0 = *reinterpret_cast<const uint32_t*>(t), t1 = *reinterpret_cast<const uint32_t*>(t + 8);
                     sv[0].r[k] = __builtin_amdgcn_perm(t1, t0, sel);
                 }
             } else {
@@ -946,7 +952,10 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
             for (int u = 0; u < 8; ++u) {
                 float4v o;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = fmaf(HP == 1 ? fmaf(dpp<kRor8>(acc[u][i]), kLoShrink, acc[u][i]) : acc[u][i] + dpp<kRor8>(acc[u][i]), kValueUnscale, zz[u >> 1]);
+                for (int i = 0; i < 4; ++i) {
+                    const float remainders = dpp<kRor8>(acc[u][i]);
+                    o[i] = fmaf(HP == 1 ? fmaf(remainders, kLoShrink, acc[u][i]) : acc[u][i] + remainders, kValueUnscale, zz[u >> 1]);
+                }
                 if (holds(u) && head >= g0 && head < g0 + HR) *reinterpret_cast<float4v*>(&sm_o[wave][head - g0][u * 16 + kb * 4]) = o;
             }
             lds_barrier();
