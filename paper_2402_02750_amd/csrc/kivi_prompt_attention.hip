@@ -501,7 +501,7 @@ Plan plan_of(const PromptParams& p) {
     // (124 workgroups of 128 rows, 4 heads x 3900 tokens: 79.8 us, in rows of 32 50.6; 64 of them, 2000 tokens: 44.4, 25.9; 160, 2 x 600, 16 / 8 heads: 18.0,
     // 21.9; 220, 7000 tokens, window 500: 24.0, 44.3)
     plan.small = pairs * ((rows + 127) / 128) <= kComputeUnits / 2;
-    if (plan.small) {
+    if (plan.small && rows > 0) {
         // keys that a tile of rows sees at most, in tiles
         int64_t keys = p.max_k;
         if (p.window > 0) keys = std::min<int64_t>(keys, (int64_t)p.window + kWaveRows + std::min(p.sinks, p.max_k));

@@ -118,6 +118,13 @@ def test_prompt_workspace(lib):
     assert lib.kivi_prompt_workspace_bytes(ctypes.byref(big), ctypes.byref(n)) == 0 and n.value == 0
 
 
+@pytest.mark.parametrize("max_q,max_k", [(0, 100), (0, 0), (5, 0), (0, 100000)])
+def test_prompt_workspace_without_rows(lib, max_q, max_k):
+    p = _prompt(batch=1, n_q_heads=4, n_kv_heads=4, max_q=max_q, max_k=max_k)
+    n = ctypes.c_size_t(1)
+    assert lib.kivi_prompt_workspace_bytes(ctypes.byref(p), ctypes.byref(n)) == 0 and n.value == 0
+
+
 def _layout(**kw):
     return _set(kivi.make_paged_layout(4, 8, 2, 2, 64, 64, 10, 96), kw)
 
@@ -130,7 +137,7 @@ def test_paged_sizes(lib):
     assert kivi.kivi_paged_sizes(_layout(bits=4)).pages == 10 * 2 * 2 * (1024 + 4096)
     assert lib.kivi_paged_sizes(ctypes.byref(_layout()), None) == INVALID
     huge = kivi.kivi_paged_sizes(_layout(n_pages=1 << 20, n_kv_heads=8, page_tokens=256))
-    assert huge.pages == (1 << 20) * 8 * 8 * 3072
+    assert huge.pages == (1 << 20) * 8 * 8 * (1024 + 2048)
 
 
 @pytest.mark.parametrize("kw,status", [
