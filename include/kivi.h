@@ -366,7 +366,8 @@ int kivi_stream_read_probe(const void* src, size_t bytes, void* sink, void* stre
 
 /* A tensor of 16-bit elements: element (b, h, t, c), c < 128, at data[b*stride_b + h*stride_h + t*stride_t + c]
  * (strides in elements, multiples of 8, not negative; data 16-byte aligned).  Tensors of rows use t as the
- * row and b = 0. */
+ * row and b = 0.  Tensors that are read may repeat (strides of 0); in those that are written every stride but the smallest
+ * steps over all that is inside it. */
 typedef struct kivi_tensor {
     void *data;
     int64_t stride_b, stride_h, stride_t;

@@ -3,7 +3,9 @@
 #include "kivi_paged.h"
 #include "kivi_prompt.h"
 
+#include <algorithm>
 #include <cmath>
+#include <utility>
 
 using namespace kivi;
 
@@ -20,10 +22,17 @@ int check_read(const kivi_tensor_t& t) {
     if (t.stride_b < 0 || t.stride_h < 0 || t.stride_t < 0 || ((t.stride_b | t.stride_h | t.stride_t) & 7)) return KIVI_ERR_INVALID_ARG;
     return KIVI_OK;
 }
-// ... that is written: no two heads, rows or batch entries at one place
+// ... that is written: no two heads, rows or batch entries at one place (whichever of the three is the innermost, each steps over all of the one inside)
 int check_written(const kivi_tensor_t& t, int64_t batch, int64_t heads, int64_t rows) {
     if (const int st = check_read(t)) return st;
-    if ((heads > 1 && t.stride_h < kHeadDim) || (rows > 1 && t.stride_t < kHeadDim) || (batch > 1 && t.stride_b < kHeadDim)) return KIVI_ERR_INVALID_ARG;
+    std::pair<int64_t, int64_t> dims[3] = {{t.stride_b, batch}, {t.stride_h, heads}, {t.stride_t, rows}};
+    std::sort(dims, dims + 3);
+    __int128 span = kHeadDim;
+    for (const auto& [stride, n] : dims)
+        if (n > 1) {
+            if (stride < span) return KIVI_ERR_INVALID_ARG;
+            span += (__int128)stride * (n - 1);
+        }
     return KIVI_OK;
 }
 int check_rotation(const kivi_rotation_t* r, bool positions_needed) {
@@ -133,7 +142,7 @@ int kivi_prompt_attention(const kivi_prompt_t* prompt, const kivi_tensor_t* q, c
     for (const kivi_tensor_t* t : {q, k, v})
         if (t == q || t->data || !no_keys)
             if (const int st = check_read(*t)) return st;
-    if (const int st = check_written(*out, prompt->q_starts ? 1 : prompt->batch, prompt->n_q_heads, prompt->max_q)) return st;
+    if (const int st = check_written(*out, prompt->q_starts ? 1 : prompt->batch, prompt->n_q_heads, prompt->q_starts ? prompt->q_rows : prompt->max_q)) return st;
     PromptParams p = prompt_params(prompt);
     p.q = tensor_params(*q); p.k = tensor_params(*k); p.v = tensor_params(*v); p.out = tensor_params(*out);
     if (workspace && workspace_bytes < prompt_workspace_bytes(p)) return KIVI_ERR_WORKSPACE;

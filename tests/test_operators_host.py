@@ -118,6 +118,33 @@ def test_prompt_workspace(lib):
     assert lib.kivi_prompt_workspace_bytes(ctypes.byref(big), ctypes.byref(n)) == 0 and n.value == 0
 
 
+@pytest.mark.parametrize("strides,sizes,status", [
+    # b, h, t; batch, heads, rows.  (without a device a call that passes the checks ends with an error of the runtime)
+    ((0, 128, 256), (1, 4, 3), INVALID),                # the second row over the third head of the first
+    ((0, 128, 512), (1, 4, 3), None), ((0, 1024, 128), (1, 4, 8), None), ((0, 896, 128), (1, 4, 8), INVALID),
+    ((1024, 128, 512), (2, 4, 3), INVALID), ((1536, 128, 512), (2, 4, 3), None), ((512, 128, 1024), (2, 4, 3), None),
+    ((0, 128, 0), (1, 4, 1), None), ((1 << 62, 128, 512), (2, 4, 1), None),
+])
+def test_outputs_that_overlap(lib, strides, sizes, status):
+    import torch
+    if status is None and torch.cuda.is_available():
+        pytest.skip("the buffers are made up")
+    b, h, t = strides
+    batch, heads, rows = sizes
+    out = kivi.kivi_tensor_t(0x1000, b, h, t)
+    p = _prompt(batch=batch, n_q_heads=heads, n_kv_heads=heads, max_q=rows, max_k=10)
+    x = kivi.kivi_tensor_t(0x1000, 0, 128, 128 * heads)
+    status_of = lib.kivi_prompt_attention(ctypes.byref(p), ctypes.byref(x), ctypes.byref(x), ctypes.byref(x), ctypes.byref(out), None, 0, None)
+    assert status_of == (kivi.KIVI_ERR_HIP if status is None else status)
+
+
+def test_rows_without_an_order(lib):
+    """Sequences of one query each: their rows have to be apart all the same."""
+    x, out = _tensor(), kivi.kivi_tensor_t(0x1000, 0, 128, 0)
+    p = _prompt(batch=3, n_q_heads=1, n_kv_heads=1, max_q=1, max_k=4, q_starts=0x5000, q_rows=3)
+    assert lib.kivi_prompt_attention(ctypes.byref(p), *[ctypes.byref(x)] * 3, ctypes.byref(out), None, 0, None) == INVALID
+
+
 @pytest.mark.parametrize("max_q,max_k", [(0, 100), (0, 0), (5, 0), (0, 100000)])
 def test_prompt_workspace_without_rows(lib, max_q, max_k):
     p = _prompt(batch=1, n_q_heads=4, n_kv_heads=4, max_q=max_q, max_k=max_k)
