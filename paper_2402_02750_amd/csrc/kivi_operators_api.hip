@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <utility>
 
 using namespace kivi;
@@ -16,7 +17,18 @@ bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0;
 int hip_status(hipError_t e) { return e == hipSuccess ? KIVI_OK : e == hipErrorNotSupported ? KIVI_ERR_UNSUPPORTED : e == hipErrorInvalidValue ? KIVI_ERR_INVALID_ARG : KIVI_ERR_HIP; }
 bool known_type(int t) { return t == KIVI_TYPE_FP16 || t == KIVI_TYPE_BF16; }
 
-// a tensor of `heads` heads that is read; strides may be 0 (broadcast)
+// a product of counts, if it is at most `limit`
+bool fits(int64_t limit, std::initializer_list<int64_t> counts) {
+    __int128 product = 1;
+    for (const int64_t n : counts) {
+        product *= n;
+        if (product > limit) return false;
+    }
+    return true;
+}
+constexpr int64_t kMaxBytes = (int64_t)1 << 62;
+
+// a tensor that is read; strides may be 0 (broadcast)
 int check_read(const kivi_tensor_t& t) {
     if (!t.data || !aligned16(t.data)) return KIVI_ERR_INVALID_ARG;
     if (t.stride_b < 0 || t.stride_h < 0 || t.stride_t < 0 || ((t.stride_b | t.stride_h | t.stride_t) & 7)) return KIVI_ERR_INVALID_ARG;
@@ -57,6 +69,8 @@ int check_prompt(const kivi_prompt_t* p) {
     if (p->max_q < 0 || p->max_k < 0 || p->window < 0 || p->sinks < 0 || !std::isfinite(p->softmax_scale)) return KIVI_ERR_INVALID_ARG;
     if (!aligned4(p->q_starts) || !aligned4(p->k_starts) || (p->q_starts && p->q_rows < 0) || (p->k_starts && p->k_rows < 0)) return KIVI_ERR_INVALID_ARG;
     if (p->head_dim != kHeadDim || !known_type(p->type)) return KIVI_ERR_UNSUPPORTED;
+    // (counted in 32 bits)
+    if (!fits(0x7fffffff, {p->batch, p->n_kv_heads}) || !fits(0x3fffffff, {p->max_q, p->n_q_heads / p->n_kv_heads})) return KIVI_ERR_UNSUPPORTED;
     return KIVI_OK;
 }
 PromptParams prompt_params(const kivi_prompt_t* p) {
@@ -76,6 +90,9 @@ int check_paged_layout(const kivi_paged_layout_t* l) {
     if (l->residual % kTileTokens != 0 || l->cap_r_tokens % kTileTokens != 0 || l->cap_r_tokens < (int64_t)l->residual + kTileTokens) return KIVI_ERR_INVALID_ARG;
     if (l->page_tokens < kTileTokens || l->page_tokens > 4096 || (l->page_tokens & (l->page_tokens - 1))) return KIVI_ERR_INVALID_ARG;
     if (l->n_q_heads / l->n_kv_heads > kMaxRepTotal || l->cap_r_tokens > 1 << 20) return KIVI_ERR_UNSUPPORTED;
+    if (!fits(kMaxBytes, {l->n_pages, l->n_kv_heads, l->page_tokens / kTileTokens, record_bytes(l->bits)}) ||
+        !fits(kMaxBytes, {l->max_sequences, l->n_kv_heads, l->cap_r_tokens, kHeadDim * 2}))
+        return KIVI_ERR_UNSUPPORTED;
     return KIVI_OK;
 }
 int check_paged(const kivi_paged_layout_t* l, const kivi_paged_cache_t* c, const kivi_paged_batch_t* b) {
@@ -84,6 +101,7 @@ int check_paged(const kivi_paged_layout_t* l, const kivi_paged_cache_t* c, const
     if (b->batch < 1 || b->max_pages < 0 || b->page_table_stride < b->max_pages || !b->lengths) return KIVI_ERR_INVALID_ARG;
     if ((b->max_pages > 0 && !b->page_table) || !aligned4(b->page_table) || !aligned4(b->lengths) || !aligned4(b->slots)) return KIVI_ERR_INVALID_ARG;
     if ((int64_t)b->max_pages * l->page_tokens > 0x7fffffff) return KIVI_ERR_INVALID_ARG;
+    if (!fits(0x7fffffff, {b->batch, l->n_q_heads})) return KIVI_ERR_UNSUPPORTED;
     return KIVI_OK;
 }
 void paged_params(const kivi_paged_layout_t* l, const kivi_paged_cache_t* c, const kivi_paged_batch_t* b, PagedParams& p) {

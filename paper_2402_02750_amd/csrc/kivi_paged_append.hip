@@ -228,8 +228,10 @@ hipError_t launch_paged_append(const PagedAppendParams& params, hipStream_t stre
     p.tokens = queries ? p.max_new : std::min(p.max_new, p.residual + kTileTokens - 1);      // (rows that stay, at most)
     p.row_heads = (queries ? p.n_q_heads : 0) + 2 * p.n_kv_heads;
     p.pieces = (p.row_heads + 7) / 8;
-    const int64_t groups = (int64_t)p.batch * p.groups * p.n_kv_heads * 2, rows = (int64_t)p.batch * p.tokens * p.pieces;
-    if (groups + rows > 0x7ffffff0) return hipErrorNotSupported;
+    // (batch times heads fits 31 bits)
+    const int64_t groups = (int64_t)p.batch * p.n_kv_heads * p.groups * 2, rows_each = (int64_t)p.batch * p.pieces;
+    if (rows_each > 0x7fffffff || groups + rows_each * p.tokens > 0x7ffffff0) return hipErrorNotSupported;
+    const int64_t rows = rows_each * p.tokens;
     p.group_waves = (int32_t)groups;
     p.row_waves = (int32_t)rows;
     p.group_blocks = (int32_t)((groups + 3) / 4);

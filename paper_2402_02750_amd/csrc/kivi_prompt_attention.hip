@@ -523,10 +523,10 @@ size_t prompt_workspace_bytes(const PromptParams& p) {
 hipError_t launch_prompt_attention(const PromptParams& params, void* workspace, size_t workspace_bytes, hipStream_t stream) {
     Args p{};
     static_cast<PromptParams&>(p) = params;
-    // (the copies' lane offsets are 32 bits over 16 rows; rows are counted in 31 bits)
+    // (the copies' lane offsets are 32 bits over 16 rows)
     const int rep = p.n_q_heads / p.n_kv_heads;
     const int64_t rows = (int64_t)p.max_q * rep, pairs = (int64_t)p.batch * p.n_kv_heads;
-    if (p.k.stride_t >= 1 << 26 || p.v.stride_t >= 1 << 26 || rows > 0x3fffffff || pairs > 0x7fffffff) return hipErrorNotSupported;
+    if (p.k.stride_t >= 1 << 26 || p.v.stride_t >= 1 << 26) return hipErrorNotSupported;
     Plan plan = plan_of(p);
     if (!workspace || workspace_bytes < prompt_workspace_bytes(p)) plan.splits = 1;
     const int tile_rows = plan.small ? kWaveRows : kWaves * kWaveRows;

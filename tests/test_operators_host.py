@@ -284,3 +284,23 @@ def test_stream_of_another_device():
     with pytest.raises(kivi.KiviError) as e:
         kivi._stream_handle(Stream(), 0)
     assert e.value.status == INVALID
+
+
+def test_products_of_counts(lib):
+    """Counts whose product leaves the integers it is held in are refused, not wrapped."""
+    n, most = ctypes.c_size_t(0), 2 ** 31 - 1
+    for kw in (dict(batch=most, n_q_heads=most, n_kv_heads=most), dict(batch=65536, n_kv_heads=65536, n_q_heads=65536), dict(max_q=most, n_q_heads=8, n_kv_heads=1)):
+        assert lib.kivi_prompt_workspace_bytes(ctypes.byref(_prompt(**kw)), ctypes.byref(n)) == UNSUPPORTED
+    sizes = kivi.kivi_paged_sizes_t()
+    for kw in (dict(n_pages=most, n_q_heads=most, n_kv_heads=most), dict(max_sequences=most, n_q_heads=1 << 30, n_kv_heads=1 << 30, cap_r_tokens=1 << 20)):
+        assert lib.kivi_paged_sizes(ctypes.byref(_layout(**kw)), ctypes.byref(sizes)) == UNSUPPORTED
+    cache = kivi.kivi_paged_cache_t(0x1000, 0x1000, 0x1000)
+    batch = kivi.kivi_paged_batch_t(1 << 20, 4, 4, 0x1000, 0x1000, None)
+    query = kivi.kivi_paged_query_t(0x1000, 0x1000, 0, 0, 0, 0.1)
+    wide = _layout(n_q_heads=1 << 12, n_kv_heads=1 << 12)
+    assert lib.kivi_paged_attention(ctypes.byref(wide), ctypes.byref(cache), ctypes.byref(batch), ctypes.byref(query), ctypes.c_void_p(0x1000), 1 << 40, None) == UNSUPPORTED
+    x = _tensor()
+    for max_new, rows in ((most, most), (1 << 24, most)):
+        batch = kivi.kivi_paged_batch_t(1 << 16, 4, 4, 0x1000, 0x1000, None)
+        new = kivi.kivi_paged_rows_t(x, x, kivi.kivi_tensor_t(), kivi.kivi_tensor_t(), 0, rows, max_new, 0x1000, None)
+        assert lib.kivi_paged_append(ctypes.byref(_layout(n_q_heads=1 << 14, n_kv_heads=1 << 14)), ctypes.byref(cache), ctypes.byref(batch), ctypes.byref(new), None) == UNSUPPORTED
