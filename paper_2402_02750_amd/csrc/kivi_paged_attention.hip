@@ -5,7 +5,7 @@
 // wavefront.  Every workgroup adds up the lengths by itself (sums across lanes without LDS) and takes one interval of the axis, so the
 // device is divided evenly whatever the lengths, and nothing but the batch's size is known to the host: a captured call follows lengths and
 // pages.  Where no piece gets longer (few units, short ones), each unit is cut evenly on its own instead, and no workgroup
-// enters two: 8 sequences of 500 tokens, 32 / 8 heads 20.6 -> 13.2 us.  A unit that lies in one interval is written out by it; of one that several
+// enters two: 8 sequences of 500 tokens, 32 / 8 heads 20.6 -> 12.6 us.  A unit that lies in one interval is written out by it; of one that several
 // share each leaves a part (maximum, sum, outputs) in the workspace, and the last to come joins them.  A workgroup shares its first and its
 // last unit at most, so the workspace has two parts per workgroup whatever the batch; a unit is counted where its first workgroup is.  Entering and leaving
 // a unit has its place on the axis too, in front of the unit's steps; an interval that begins in it begins with the steps.
@@ -56,8 +56,9 @@ constexpr int kWorkgroups = 768;       // three per compute unit; a multiple of 
 // 0, 2, 3, 4 with rows 1; 0, 2, 3 with rows 2: 64 x 500-8000 tokens, 32 / 8 heads -, 60, 58.6, 61; 66, 61, 63 us; 200 x 500-2000 -, 63, 61, 64; 67, 66, 64;
 // 64 x 500-8000, 64 / 8 -, 71, 66, 67; 73, 70, 71.)
 constexpr int kUnitCost = 3;
-// Steps of an interval, at least (1, 2, 4, 8: one sequence of 3001 tokens 15.3, 15.3, 18.2, 25 us; 4 heads x 1023 tokens 11.0, 9.9, 11.7, 17; 8000 tokens,
-// 32 / 8 heads 21.9, 18.0, 20.7, 26)
+constexpr int kJoined = 8;             // parts that are loaded at a time where they are joined
+// Steps of an interval, at least; 1 where units have kJoined steps or fewer.  (1, 2, 3: 8 sequences of 500 tokens, 32 / 8 heads 12.5, 14.2, 15.9 us; 4 heads x 1023
+// tokens 10.9, 9.6, 11.1; 8000 tokens, 32 / 8 heads 20.9, 18.4, 19.3; one sequence of 3001 tokens, 32 / 8 heads 15.6, 14.9, 16.8.)
 constexpr int kMinCost = 2;
 constexpr int kScanned = 4;            // times 64 sequences whose costs stay in registers
 constexpr int kMaxHeads = 8;           // query heads of a unit
@@ -300,6 +301,10 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
                 else low = mid + 1;
             }
             length = low;
+            bool few = length == kMinCost;
+#pragma unroll
+            for (int i = 0; i < kScanned; ++i) few = few && !__any(costs[i] > kJoined);
+            if (few && fits(1)) length = 1;
         }
     }
     // what of the axis is in front of a sequence: workgroups with pieces of their own, cost otherwise
@@ -988,28 +993,27 @@ __global__ __launch_bounds__(64 * kWaves, 3) void paged_attention_kernel(Args p)
             if (sm_last) {
                 // the unit is the first one of every workgroup but, maybe, the first of them
                 const int second = !own_pieces && owner0 * length < here.unit0 - unit_cost ? 1 : 0;
-                constexpr int kBatch = 8;
                 for (int hh = wave; hh < live; hh += kWaves) {
                     float mm = kNothing, sum = 0.f, ox = 0.f, oy = 0.f;
 #pragma unroll 1
-                    for (int g0 = 0; g0 < parts; g0 += kBatch) {
-                        float2 st[kBatch], o2[kBatch];
+                    for (int g0 = 0; g0 < parts; g0 += kJoined) {
+                        float2 st[kJoined], o2[kJoined];
 #pragma unroll
-                        for (int g = 0; g < kBatch; ++g) {
+                        for (int g = 0; g < kJoined; ++g) {
                             const int at = min(g0 + g, parts - 1), part = (owner0 + at) * 2 + (at == 0 ? second : 0);
                             st[g] = load_shared(p.part_ml + ((int64_t)part * kMaxHeads + hh) * 2);
                             o2[g] = load_shared(p.part_o + ((int64_t)part * kMaxHeads + hh) * kPartFloats + c2);
                         }
                         float mn = mm;
 #pragma unroll
-                        for (int g = 0; g < kBatch; ++g) mn = fmaxf(mn, st[g].x);
+                        for (int g = 0; g < kJoined; ++g) mn = fmaxf(mn, st[g].x);
                         const float f0 = __builtin_amdgcn_exp2f(mm - mn);
                         mm = mn;
                         sum *= f0;
                         ox *= f0;
                         oy *= f0;
 #pragma unroll
-                        for (int g = 0; g < kBatch; ++g) {
+                        for (int g = 0; g < kJoined; ++g) {
                             const float f = g0 + g < parts ? __builtin_amdgcn_exp2f(st[g].x - mn) : 0.f;
                             sum = fmaf(st[g].y, f, sum);
                             ox = fmaf(o2[g].x, f, ox);
