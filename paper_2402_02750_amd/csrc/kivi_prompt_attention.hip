@@ -15,15 +15,15 @@
 // Probabilities are rounded to the tensors' type, to nearest: an error of 2^-12 (bf16: 2^-9) of each term at most.
 //
 // Two kernels.  prompt_tiles_kernel: a workgroup has 128 rows and walks over tiles of 64 keys that its four wavefronts share.
-// prompt_rows_kernel, where those workgroups would not fill the device: 32 rows, the wavefronts take the tiles (of 32 keys) in turn, each with buffers
-// of its own and without barriers, and join in LDS; with a workspace, several workgroups share the keys of the same rows, and a second launch joins them.
+// prompt_rows_kernel, where those workgroups would not fill the device or would have 32 rows at most: 32 rows, and one to four wavefronts that take the tiles
+// (of 32 keys) in turn, each with buffers of its own and without barriers, and join in LDS; with a workspace, several workgroups share the keys of the same rows, and a second launch joins them.
 //
 // Tiles arrive by asynchronous copies into two buffers of keys and two of values, one tile ahead; the logits of the next tile are asked for before the
 // exponentials of this one, and its maximum before the barrier.  In LDS the 16-byte pieces of a row change place so that no read has bank conflicts.
 // Bound: the card's power.  4 x 4096 tokens, 32 / 8 heads, bf16 546 us, 1.01 PFLOP/s (a library product of 8192^3 1.19); on zeros instead of normal numbers it
 // runs in 414 us (the product: 1.76 PFLOP/s).  The clock is at 1.8 of 2.4 GHz, matrix instructions take half of the cycles, vector ones 40 %.  What did not help:
 // interleaving the two by hand (598-619 us), wavefront priorities (583-594), sums of probabilities by dot products (550), eight wavefronts per workgroup (559),
-// the workgroups of one pair after another (555).  8001 tokens, window 2048 and 4 first keys, fp16 263 us (0.89 PFLOP/s); 1001 tokens, 4 heads 14.8.
+// the workgroups of one pair after another (555).  8001 tokens, window 2048 and 4 first keys, fp16 263 us (0.89 PFLOP/s); 1001 tokens, 4 heads 13.6.
 #include "kivi_prompt.h"
 
 #include <algorithm>
@@ -38,9 +38,10 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 4, kWaveRows = 32, kRowBytes = kHeadDim * 2;
 constexpr int kComputeUnits = 256;
-// Tiles per wavefront, at least, before the keys of a tile of rows are split.  (One query, 8000 keys before it, 32 / 8 heads, and five queries, 7000 keys,
-// 4 heads: not split 84 and 73 us; 2: 19.4, 17.5; 4: 18.5, 17.0; 8: 22.4, 22.3.)
-constexpr int kSplitTiles = 4;
+// Tiles per wavefront from which the keys of a tile of rows are split, and how many are left then, at least.  (One query, 8000 keys before it, 32 / 8 heads, and
+// five queries, 7000 keys, 4 heads: not split 84 and 73 us; left 2: 19.4, 17.5; 4: 18.5, 17.0; 8: 22.4, 22.3.  One query, 32 / 8 heads after 1000, 1500, 2000
+// keys, not split 14.7, 18.7, 23.0, split 16.5, 16.7, 16.8, which is the second launch and the binding's workspace.)
+constexpr int kSplitTiles = 4, kSplitFrom = 10;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.f;                  // log2 headroom of the running maximum
 constexpr float kNothing = -1e30f;             // running maximum of a row that has seen nothing
@@ -377,11 +378,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_tiles_kernel(Args p) {
     }
 }
 
-template <bool BF16>
-__global__ __launch_bounds__(64 * kWaves, 1) void prompt_rows_kernel(Args p) {
+template <bool BF16, int W>
+__global__ __launch_bounds__(64 * W, 1) void prompt_rows_kernel(Args p) {
     constexpr int kKeys = 32, kTileBytes = kKeys * kRowBytes;
-    __shared__ __align__(16) unsigned char sm[kWaves][2][2][kTileBytes];  // [wavefront][buffer][keys, values]; then outputs [wavefront][channel][row]
-    __shared__ float sm_ml[kWaves][2][kWaveRows];
+    __shared__ __align__(16) unsigned char sm[W][2][2][kTileBytes];  // [wavefront][buffer][keys, values]; then outputs [wavefront][channel][row]
+    __shared__ float sm_ml[W][2][kWaveRows];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int pair, tile;
@@ -392,7 +393,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void prompt_rows_kernel(Args p) {
     Rows<BF16, 1> r;
     r.start(p, w, w.row0 + col, half);
     const Tiles<kKeys> tiles(p, w);
-    // this workgroup's tiles: [from, to), of them every fourth
+    // this workgroup's tiles: [from, to), of which the wavefronts take turns
     const int from = (int)((int64_t)tiles.count * split / p.splits), to = (int)((int64_t)tiles.count * (split + 1) / p.splits);
     Copier<KeySwap> keys(base_of(p.k, p.k_starts, w), p.k.stride_t, 0, 16, lane, KeySwap{});
     Copier<ValueSwap> values(base_of(p.v, p.k_starts, w), p.v.stride_t, 0, 16, lane, ValueSwap{});
@@ -408,10 +409,10 @@ __global__ __launch_bounds__(64 * kWaves, 1) void prompt_rows_kernel(Args p) {
     };
     int buffer = 0;
     if (from + wave < to) copy_tile(from + wave, 0);
-    for (int i = from + wave; i < to; i += kWaves) {
-        if (i + kWaves < to) {
+    for (int i = from + wave; i < to; i += W) {
+        if (i + W < to) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the other buffer's last reads are done
-            copy_tile(i + kWaves, buffer ^ 1);
+            copy_tile(i + W, buffer ^ 1);
             asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
         } else {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -437,35 +438,39 @@ __global__ __launch_bounds__(64 * kWaves, 1) void prompt_rows_kernel(Args p) {
         sm_ml[wave][1][col] = lw;
     }
     __syncthreads();
-    // wavefront cb has channels 32 cb + 16 half .. of all rows
-    float m = kNothing, l = 0.f, f[kWaves], o[16];
+    // 32 channels after the other, this wavefront's first (half: the upper sixteen), of all rows
+    float m = kNothing, l = 0.f, f[W];
 #pragma unroll
-    for (int x = 0; x < kWaves; ++x) m = fmaxf(m, sm_ml[x][0][col]);
+    for (int x = 0; x < W; ++x) m = fmaxf(m, sm_ml[x][0][col]);
 #pragma unroll
-    for (int x = 0; x < kWaves; ++x) {
+    for (int x = 0; x < W; ++x) {
         f[x] = __builtin_amdgcn_exp2f(sm_ml[x][0][col] - m);
         l = fmaf(sm_ml[x][1][col], f[x], l);
     }
-    const int c0 = wave * 32 + half * 16;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        o[e] = 0.f;
-#pragma unroll
-        for (int x = 0; x < kWaves; ++x) o[e] = fmaf(reinterpret_cast<const float*>(&sm[x][0][0][0])[(c0 + e) * kWaveRows + col], f[x], o[e]);
-    }
     const int row = w.row0 + col;
     if (row >= w.rows) return;
-    if (p.splits == 1) {
-        const float g = l > 0.f ? 1.f / l : 0.f;
-        __half* dst = out_row(p, w, row) + c0;
 #pragma unroll
-        for (int e = 0; e < 16; e += 4) store_four<BF16>(dst + e, o[e] * g, o[e + 1] * g, o[e + 2] * g, o[e + 3] * g);
-    } else {
-        const int64_t part = (((int64_t)pair * p.row_tiles + tile) * kWaveRows + col) * p.splits + split;
-        float4v* dst = reinterpret_cast<float4v*>(p.part_o + part * kHeadDim + c0);
+    for (int cb = wave; cb < 4; cb += W) {
+        const int c0 = cb * 32 + half * 16;
+        float o[16];
 #pragma unroll
-        for (int e = 0; e < 16; e += 4) dst[e / 4] = float4v{o[e], o[e + 1], o[e + 2], o[e + 3]};
-        if (c0 == 0) *reinterpret_cast<float2*>(p.part_ml + part * 2) = make_float2(m, l);
+        for (int e = 0; e < 16; ++e) {
+            o[e] = 0.f;
+#pragma unroll
+            for (int x = 0; x < W; ++x) o[e] = fmaf(reinterpret_cast<const float*>(&sm[x][0][0][0])[(c0 + e) * kWaveRows + col], f[x], o[e]);
+        }
+        if (p.splits == 1) {
+            const float g = l > 0.f ? 1.f / l : 0.f;
+            __half* dst = out_row(p, w, row) + c0;
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) store_four<BF16>(dst + e, o[e] * g, o[e + 1] * g, o[e + 2] * g, o[e + 3] * g);
+        } else {
+            const int64_t part = (((int64_t)pair * p.row_tiles + tile) * kWaveRows + col) * p.splits + split;
+            float4v* dst = reinterpret_cast<float4v*>(p.part_o + part * kHeadDim + c0);
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) dst[e / 4] = float4v{o[e], o[e + 1], o[e + 2], o[e + 3]};
+            if (c0 == 0) *reinterpret_cast<float2*>(p.part_ml + part * 2) = make_float2(m, l);
+        }
     }
 }
 
@@ -493,20 +498,26 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(Args p) {
     store_four<BF16>(out_row(p, w, row) + c, o[0] * f, o[1] * f, o[2] * f, o[3] * f);
 }
 
-// What a call runs: tiles of 128 rows, or of 32 with `splits` workgroups each
-struct Plan { bool small; int splits; };
+// What a call runs: tiles of 128 rows, or of 32 by `waves` wavefronts with `splits` workgroups each
+struct Plan { bool small; int waves, splits; };
 Plan plan_of(const PromptParams& p) {
     const int64_t rows = (int64_t)p.max_q * (p.n_q_heads / p.n_kv_heads), pairs = (int64_t)p.batch * p.n_kv_heads;
-    Plan plan{false, 1};
+    const int64_t groups = pairs * ((rows + kWaveRows - 1) / kWaveRows);
+    Plan plan{false, kWaves, 1};
+    if (rows == 0) return plan;
     // (124 workgroups of 128 rows, 4 heads x 3900 tokens: 79.8 us, in rows of 32 50.6; 64 of them, 2000 tokens: 44.4, 25.9; 160, 2 x 600, 16 / 8 heads: 18.0,
     // 21.9; 220, 7000 tokens, window 500: 24.0, 44.3)
-    plan.small = pairs * ((rows + 127) / 128) <= kComputeUnits / 2;
-    if (plan.small && rows > 0) {
+    plan.small = rows <= kWaveRows || pairs * ((rows + 127) / 128) <= kComputeUnits / 2;
+    // One tile of rows per pair leaves three wavefronts of a 128-row workgroup idle.  Four wavefronts take a compute unit's LDS, so more workgroups than
+    // compute units have two each, or one.  (128 rows, 4, 2, 1 wavefronts: 288 pairs, 5 tokens after 315 16.0, 18.4, 13.8, 16.8 us; 512, 20 after 500 28.1, 29.4,
+    // 26.0, 26.3; 1600, 32 / 8 heads, 1 after 100 28.6, 36.4, 27.8, 22.8; 1888, 13 tokens 23.3, 37.6, 20.0, 12.5)
+    if (rows <= kWaveRows) plan.waves = groups <= kComputeUnits ? 4 : groups <= 2 * kComputeUnits ? 2 : 1;
+    if (plan.small) {
         // keys that a tile of rows sees at most, in tiles
         int64_t keys = p.max_k;
         if (p.window > 0) keys = std::min<int64_t>(keys, (int64_t)p.window + kWaveRows + std::min(p.sinks, p.max_k));
-        const int64_t tiles = (keys + 31) / 32, groups = pairs * ((rows + 31) / 32);
-        plan.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kComputeUnits / groups, tiles / (kWaves * kSplitTiles)));
+        const int64_t tiles = (keys + 31) / 32;
+        if (tiles >= kWaves * kSplitFrom) plan.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kComputeUnits / groups, tiles / (kWaves * kSplitTiles)));
     }
     return plan;
 }
@@ -544,8 +555,11 @@ hipError_t launch_prompt_attention(const PromptParams& params, void* workspace, 
     }
     p.part_o = static_cast<float*>(workspace);
     p.part_ml = p.part_o + (size_t)pairs * p.row_tiles * kWaveRows * plan.splits * kHeadDim;
-    if (p.bf16) prompt_rows_kernel<true><<<(unsigned)blocks, 64 * kWaves, 0, stream>>>(p);
-    else prompt_rows_kernel<false><<<(unsigned)blocks, 64 * kWaves, 0, stream>>>(p);
+#define KIVI_ROWS(W) p.bf16 ? prompt_rows_kernel<true, W><<<(unsigned)blocks, 64 * W, 0, stream>>>(p) : prompt_rows_kernel<false, W><<<(unsigned)blocks, 64 * W, 0, stream>>>(p)
+    if (plan.waves == 4) KIVI_ROWS(4);
+    else if (plan.waves == 2) KIVI_ROWS(2);
+    else KIVI_ROWS(1);
+#undef KIVI_ROWS
     if (const hipError_t e = hipGetLastError(); e != hipSuccess || plan.splits == 1) return e;
     const int64_t join_blocks = pairs * p.row_tiles * kWaveRows / 8;
     if (p.bf16) prompt_join_kernel<true><<<(unsigned)join_blocks, 256, 0, stream>>>(p);

@@ -109,6 +109,36 @@ def test_ragged_batches(dtype, window, sinks):
     assert (out[q_starts[-2]:q_starts[-1]] == 5).all() and torch.equal(out[:q_starts[-2]], want[:q_starts[-2]])
 
 
+@pytest.mark.parametrize("batch,q_heads,kv_heads,n_q,n_k,dtype,window,sinks", [
+    (9, 32, 32, 5, 75, "fp16", 0, 0),           # 288 tiles of rows
+    (21, 32, 32, 3, 130, "bf16", 40, 3),        # 672
+    (40, 32, 16, 16, 333, "fp16", 0, 0),        # 640, all 32 rows of each
+    (22, 24, 24, 1, 1, "fp16", 0, 0),
+    (24, 24, 12, 7, 0, "bf16", 0, 0),
+])
+def test_many_sequences_of_few_rows(batch, q_heads, kv_heads, n_q, n_k, dtype, window, sinks):
+    test_uniform_batches(batch, q_heads, kv_heads, n_q, n_k, dtype, window, sinks)
+
+
+@pytest.mark.parametrize("sequences,kv_heads", [(40, 8), (70, 8)])
+def test_many_ragged_sequences_of_few_rows(sequences, kv_heads):
+    torch = gh.require_gpu()
+    print(f"case prompt ragged few rows {sequences} x {kv_heads}", flush=True)
+    rng, gen = np.random.default_rng(sequences), torch.Generator(device="cuda").manual_seed(sequences)
+    n_q = rng.integers(0, 9, sequences)
+    n_k = n_q + rng.integers(0, 200, sequences) * rng.integers(0, 2, sequences)
+    q_starts, k_starts = np.cumsum(np.r_[0, n_q]), np.cumsum(np.r_[0, n_k])
+    heads = 4 * kv_heads
+    q, k, v = (torch.randn(int(n), h, 128, device="cuda", generator=gen, dtype=torch.float16) for n, h in ((q_starts[-1], heads), (k_starts[-1], kv_heads), (k_starts[-1], kv_heads)))
+    out = torch.full_like(q, 5.0)
+    starts = [torch.tensor(s, dtype=torch.int32, device="cuda") for s in (q_starts, k_starts)]
+    kivi.kivi_prompt_attention(q, k, v, out, 0.09, *starts, max_q=8, max_k=int(n_k.max()))
+    torch.cuda.synchronize()
+    for b in range(sequences):
+        qs, ks = slice(q_starts[b], q_starts[b + 1]), slice(k_starts[b], k_starts[b + 1])
+        _check(out[qs], q[qs], k[ks], v[ks], 0.09, 0, 0, "fp16", f"sequence {b}")
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.1, 1.0])
 def test_scales(scale):
     torch = gh.require_gpu()
